@@ -398,6 +398,72 @@ hpf_status hpf_op_bn_relu_backward(hpf_dtype dtype, const void* x, const void* d
 hpf_status hpf_op_bn_relu_forward_noalloc(hpf_dtype dtype, const void* x, const float* gamma, const float* beta,
                                           float eps, void* a, void* stats, int32_t M, int32_t C, void* hip_stream);
 
+/* ---- Operators at the answer end of a model ---------------------------------------------------
+ * The matrix product with its epilogue that a dense layer or a classifier is, what an evaluation reads from logits, and
+ * the loss of a student that learns from a teacher's most likely classes; each with its gradient.  They need no partition:
+ * all tensors are the caller's (dev), row-major, with a row stride in elements (>= the row's length) where the call takes
+ * an `ld`; any alignment that the element type allows.  Sizes are any: odd ones, one row, no row (rows or M == 0: outputs
+ * without an element, sums over no rows are zero).  Every call only enqueues work, keeps nothing behind, and gives the
+ * same bits for the same inputs; it may be captured into a graph.  `workspace` (256-byte aligned, may be NULL where its
+ * size is 0) holds nothing from one call to the next; calls that can overlap in time need workspaces of their own.
+ * No output may overlap another tensor of the call except where a call says so.
+ *
+ * Products.  dtype is the type of x, y, residual, slope, dy and dx; weights, bias and their gradients are fp32 masters
+ * (w [K][N]).  HPF_BF16: the products take bf16 copies of the weights, which hpf_op_linear_pack lays out once after every
+ * change of w (2 * (N * ceil64(K) + K * ceil64(N)) bytes, 256-byte aligned), and sum in fp32.  HPF_F32 (check mode): `weights`
+ * is w itself, products and sums are in double.
+ *   M <= 2^22, K, N <= 2^20 (else HPF_EUNSUPPORTED). */
+typedef enum { HPF_ACT_NONE = 0, HPF_ACT_RELU = 1, HPF_ACT_GELU = 2 /* z * Phi(z) */, HPF_ACT_SILU = 3 /* z / (1 + exp(-z)) */ } hpf_activation;
+size_t hpf_op_linear_packed_bytes(int32_t K, int32_t N);
+hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed, size_t packed_bytes, void* hip_stream);
+/* workspace of either call below for these sizes */
+size_t hpf_op_linear_workspace_bytes(hpf_dtype dtype, int32_t M, int32_t K, int32_t N);
+/* z = x[M,K] w + bias; y[M,N] = act(z) + residual; slope[M,N] (dense) = act'(z) (relu: 0 where z <= 0), from the unrounded z, for
+ * hpf_op_linear_backward.  bias, residual and slope may be NULL; residual and y may be the same tensor. */
+hpf_status hpf_op_linear_forward(hpf_dtype dtype, const void* x, int64_t ldx, const void* weights, const float* bias,
+                                 const void* residual, int64_t ldr, void* y, int64_t ldy, void* slope, int32_t M, int32_t K,
+                                 int32_t N, int32_t activation, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* dz = dy[M,N] * slope[M,N], rounded to dtype (slope NULL: dz = dy); dx[M,K] = dz w^T; dw[K,N] = x^T dz; db[N] = column sums
+ * of dz.  accumulate != 0: dw and db are added to.  dx, dw, db may be NULL (not wanted; x is read for dw only, weights for
+ * dx only).  The residual's gradient is dy. */
+hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* weights,
+                                  const void* slope, void* dx, int64_t lddx, float* dw, float* db, int32_t accumulate, int32_t M,
+                                  int32_t K, int32_t N, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Rows of logits.  dtype is the type of the logits and of gradients with respect to them; everything else is fp32 (or int32)
+ * and statistics are held in fp32 or wider.  classes <= 2^28, lists of at most 64 entries (else HPF_EUNSUPPORTED).
+ * A logit of -infinity is a masked class: probability 0, never in a list.  A row of masked classes only takes no part: log
+ * probabilities -infinity, entropy 0, loss 0, gradient 0.  A row with a NaN or +infinity gives NaN (rank and indices -1).
+ * labels: int32 in [0, classes), or -1: the row has no label (log probability 0, rank -1, no term in a loss); any other
+ * value gives NaN.
+ * workspace of hpf_op_logprob_forward and hpf_op_distill: */
+size_t hpf_op_logits_workspace_bytes(hpf_dtype dtype, int32_t rows, int32_t classes, int32_t top);
+/* Per row: logprob of the label, entropy, rank (how many classes are before the label in the order of larger logit, then
+ * lower index: rank < 5 is a top-5 hit), stats[rows][2] = {maximum, log sum exp(logit - maximum)} for the gradient, and the
+ * `top` first classes of that order, top_index[rows][top] and top_logprob[rows][top] (-1 and -infinity behind the last
+ * unmasked class).  Every output may be NULL; labels may be NULL if logprob and rank are; top == 0: no list. */
+hpf_status hpf_op_logprob_forward(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* labels, float* logprob,
+                                  float* entropy, int32_t* rank, float* stats, int32_t* top_index, float* top_logprob, int32_t top,
+                                  int32_t rows, int32_t classes, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* dlogits = grad_logprob * d logprob + grad_entropy * d entropy, from the stats and entropy of the forward call.  Either
+ * gradient may be NULL (0); entropy is read with grad_entropy only, labels with grad_logprob only.  dlogits may be the
+ * logits themselves. */
+hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* labels, const float* stats,
+                                   const float* grad_logprob, const float* entropy, const float* grad_entropy, void* dlogits,
+                                   int64_t ldd, int32_t rows, int32_t classes, void* hip_stream);
+/* Distillation.  A row's teacher gives a list of classes with their logits (or log probabilities: a shift of a row changes
+ * nothing), top_index / top_logit [rows][top]; an entry with index < 0 or logit -infinity is not there, an index >= classes
+ * gives NaN, a class listed twice counts with both.  p = softmax(top_logit / temperature) over the list, q =
+ * softmax(logits / temperature) over all classes;
+ *   loss[row] = (1 - hard_weight) * temperature^2 * sum_j p_j (log p_j - log q_j) + hard_weight * (-log softmax(logits)[label])
+ *   dlogits[row] = row_weight[row] * d loss[row] / d logits[row]
+ * in one call.  A row without entries or without label has no such term.  row_weight NULL: 1.  dlogits NULL: the loss alone.
+ * labels may be NULL if hard_weight is 0.  temperature in [1e-4, 1e4], hard_weight in [0, 1]. */
+hpf_status hpf_op_distill(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* top_index, const float* top_logit,
+                          int32_t top, const int32_t* labels, float temperature, float hard_weight, const float* row_weight,
+                          float* loss, void* dlogits, int64_t ldd, int32_t rows, int32_t classes, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
 /* ---- Measurement aids ------------------------------------------------------------------------
  * Not steps of the method: two plain kernels that say what this chip achieves, so that kernel rates can be
  * quoted against a measured ceiling next to the data-sheet one.

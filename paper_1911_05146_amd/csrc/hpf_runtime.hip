@@ -19,22 +19,25 @@
 
 #include "../../include/hpf.h"
 #include "hpf_admission.h"
+#include "hpf_error.h"
 #include "hpf_figures.h"
 #include "hpf_kernels.h"
 
 using namespace hpf;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
 
-hpf_status fail(hpf_status st, const char* fmt, ...) {
+hpf_status hpf::fail(hpf_status st, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return st;
 }
+
+namespace {
 
 constexpr size_t ALIGN = 256;
 // Regions of the micro-batches start 64 KiB apart or a multiple of that, counted from the arena's start (which is itself on 256 bytes, or better, as the caller

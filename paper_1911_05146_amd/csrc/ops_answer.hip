@@ -1,0 +1,199 @@
+// Entry points of the operators at the answer end of a model (include/hpf.h): argument checks and launches.
+#include "hpf_answer.h"
+#include "hpf_error.h"
+
+using namespace hpf;
+
+namespace {
+
+constexpr int MAX_WIDTH = 1 << 20;       // columns of a matrix
+constexpr int MAX_CLASSES = 1 << 28;
+
+bool type_of(hpf_dtype dtype, int& dt) {
+  dt = dtype == HPF_BF16 ? DT_BF16 : DT_F32;
+  return dtype == HPF_BF16 || dtype == HPF_F32;
+}
+bool rows_ok(int64_t ld, int32_t cols) { return ld >= cols && ld <= (int64_t)1 << 40; }
+size_t elem(int dt) { return dt == DT_BF16 ? 2 : 4; }
+bool element_aligned(const void* p, int dt) { return (uintptr_t)p % elem(dt) == 0; }
+// bytes that a [rows, cols] matrix with row stride ld spans
+size_t span(int dt, int64_t rows, int64_t cols, int64_t ld) { return rows ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem(dt) : 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && x < y + nb && y < x + na;
+}
+hpf_status launched(hipError_t e) { return e == hipSuccess ? HPF_OK : fail(HPF_EDEVICE, "launch failed: %s", hipGetErrorString(e)); }
+
+hpf_status linear_shape(hpf_dtype dtype, int32_t M, int32_t K, int32_t N, int& dt) {
+  if (!type_of(dtype, dt)) return fail(HPF_EINVAL, "unknown dtype");
+  if (M < 0 || K < 1 || N < 1) return fail(HPF_EINVAL, "M must not be negative, K and N must be positive (%d, %d, %d)", M, K, N);
+  if (K > MAX_WIDTH || N > MAX_WIDTH || M > (1 << 22)) return fail(HPF_EUNSUPPORTED, "more than 2^22 rows or 2^20 columns (%d, %d, %d)", M, K, N);
+  return HPF_OK;
+}
+hpf_status workspace_ok(const void* workspace, size_t bytes, size_t need) {
+  if (!need) return HPF_OK;
+  if (!workspace) return fail(HPF_EINVAL, "null workspace");
+  if ((uintptr_t)workspace % 256) return fail(HPF_EINVAL, "workspace must be 256-byte aligned");
+  if (bytes < need) return fail(HPF_ENOMEM, "workspace has %zu bytes, %zu needed", bytes, need);
+  return HPF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hpf_op_linear_packed_bytes(int32_t K, int32_t N) {
+  return K < 1 || N < 1 || K > MAX_WIDTH || N > MAX_WIDTH ? 0 : linear_packed_elems(K, N) * sizeof(bf16_t);
+}
+
+hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed, size_t packed_bytes, void* hip_stream) {
+  if (!w || !packed) return fail(HPF_EINVAL, "null tensor");
+  int dt;
+  const hpf_status st = linear_shape(HPF_BF16, 0, K, N, dt);
+  if (st != HPF_OK) return st;
+  if ((uintptr_t)packed % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
+  const size_t need = hpf_op_linear_packed_bytes(K, N);
+  if (packed_bytes < need) return fail(HPF_ENOMEM, "packed weights have %zu bytes, %zu needed", packed_bytes, need);
+  if (overlap(w, (size_t)K * N * 4, packed, need)) return fail(HPF_EINVAL, "packed weights overlap the weights");
+  return launched(launch_linear_pack(w, (bf16_t*)packed, K, N, (hipStream_t)hip_stream));
+}
+
+size_t hpf_op_linear_workspace_bytes(hpf_dtype dtype, int32_t M, int32_t K, int32_t N) {
+  int dt;
+  if (linear_shape(dtype, M, K, N, dt) != HPF_OK || M == 0) return 0;
+  return linear_workspace_bytes(dt, M, K, N);
+}
+
+hpf_status hpf_op_linear_forward(hpf_dtype dtype, const void* x, int64_t ldx, const void* weights, const float* bias,
+                                 const void* residual, int64_t ldr, void* y, int64_t ldy, void* slope, int32_t M, int32_t K,
+                                 int32_t N, int32_t activation, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int dt;
+  hpf_status st = linear_shape(dtype, M, K, N, dt);
+  if (st != HPF_OK) return st;
+  if (activation < ACT_NONE || activation > ACT_SILU) return fail(HPF_EINVAL, "unknown activation %d", activation);
+  if (M == 0) return HPF_OK;
+  if (!x || !weights || !y) return fail(HPF_EINVAL, "null tensor");
+  if (!rows_ok(ldx, K) || !rows_ok(ldy, N) || (residual && !rows_ok(ldr, N))) return fail(HPF_EINVAL, "row stride shorter than a row");
+  if (!element_aligned(x, dt) || !element_aligned(y, dt) || !element_aligned(residual, dt) || !element_aligned(slope, dt))
+    return fail(HPF_EINVAL, "tensor not aligned to its elements");
+  if (dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
+  const size_t ny = span(dt, M, N, ldy), nx = span(dt, M, K, ldx), ns = span(dt, M, N, N);
+  const size_t nw = dt == DT_BF16 ? hpf_op_linear_packed_bytes(K, N) : (size_t)K * N * 4;
+  if (overlap(x, nx, y, ny) || overlap(x, nx, slope, ns) || overlap(y, ny, slope, ns) || overlap(weights, nw, y, ny) || overlap(weights, nw, slope, ns) ||
+      (residual && (overlap(residual, span(dt, M, N, ldr), slope, ns) || (overlap(residual, span(dt, M, N, ldr), y, ny) && (residual != y || ldr != ldy)))))
+    return fail(HPF_EINVAL, "an output overlaps another tensor (only residual and y may be the same)");
+  st = workspace_ok(workspace, workspace_bytes, linear_workspace_bytes(dt, M, K, N));
+  if (st != HPF_OK) return st;
+  const LinearForward a{x, ldx, weights, bias, residual, ldr, y, ldy, slope, M, K, N, activation};
+  return launched(launch_linear_forward(dt, a, workspace, (hipStream_t)hip_stream));
+}
+
+hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* weights,
+                                  const void* slope, void* dx, int64_t lddx, float* dw, float* db, int32_t accumulate, int32_t M,
+                                  int32_t K, int32_t N, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int dt;
+  hpf_status st = linear_shape(dtype, M, K, N, dt);
+  if (st != HPF_OK) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (M == 0) {
+    if (accumulate) return HPF_OK;
+    hipError_t e = dw ? launch_zero_f32(dw, (size_t)K * N, s) : hipSuccess;
+    if (e == hipSuccess && db) e = launch_zero_f32(db, (size_t)N, s);
+    return launched(e);
+  }
+  if (!dx && !dw && !db) return HPF_OK;
+  if (!dy || (dx && !weights) || (dw && !x)) return fail(HPF_EINVAL, "null tensor");
+  if (!rows_ok(lddy, N) || (dw && !rows_ok(ldx, K)) || (dx && !rows_ok(lddx, K))) return fail(HPF_EINVAL, "row stride shorter than a row");
+  if (!element_aligned(dy, dt) || !element_aligned(x, dt) || !element_aligned(dx, dt) || !element_aligned(slope, dt))
+    return fail(HPF_EINVAL, "tensor not aligned to its elements");
+  if (dx && dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
+  const size_t ndy = span(dt, M, N, lddy), nx = dw ? span(dt, M, K, ldx) : 0, ns = slope ? span(dt, M, N, N) : 0, ndx = dx ? span(dt, M, K, lddx) : 0;
+  const size_t nw = !dx ? 0 : dt == DT_BF16 ? hpf_op_linear_packed_bytes(K, N) : (size_t)K * N * 4;
+  const struct { const void* p; size_t n; } in[] = {{dy, ndy}, {x, nx}, {slope, ns}, {weights, nw}}, out[] = {{dx, ndx}, {dw, dw ? (size_t)K * N * 4 : 0}, {db, db ? (size_t)N * 4 : 0}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& q : in)
+      if (out[i].n && q.n && overlap(out[i].p, out[i].n, q.p, q.n)) return fail(HPF_EINVAL, "an output overlaps an input");
+    for (int j = i + 1; j < 3; ++j)
+      if (out[i].n && out[j].n && overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(HPF_EINVAL, "two outputs overlap");
+  }
+  st = workspace_ok(workspace, workspace_bytes, linear_workspace_bytes(dt, M, K, N));
+  if (st != HPF_OK) return st;
+  const LinearBackward a{dy, lddy, x, ldx, weights, slope, dx, lddx, dw, db, accumulate, M, K, N};
+  return launched(launch_linear_backward(dt, a, workspace, s));
+}
+
+static hpf_status logits_shape(hpf_dtype dtype, const void* logits, int64_t ld, int32_t top, int32_t rows, int32_t classes, int& dt) {
+  if (!type_of(dtype, dt)) return fail(HPF_EINVAL, "unknown dtype");
+  if (rows < 0 || classes < 1) return fail(HPF_EINVAL, "rows must not be negative, classes must be positive (%d, %d)", rows, classes);
+  if (classes > MAX_CLASSES) return fail(HPF_EUNSUPPORTED, "more than 2^28 classes");
+  if (top < 0) return fail(HPF_EINVAL, "negative list length");
+  if (top > TOP_MAX) return fail(HPF_EUNSUPPORTED, "a list of %d entries, at most %d", top, TOP_MAX);
+  if (rows == 0) return HPF_OK;
+  if (!logits) return fail(HPF_EINVAL, "null logits");
+  if (!rows_ok(ld, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
+  if (!element_aligned(logits, dt)) return fail(HPF_EINVAL, "logits not aligned to their elements");
+  return HPF_OK;
+}
+
+size_t hpf_op_logits_workspace_bytes(hpf_dtype dtype, int32_t rows, int32_t classes, int32_t top) {
+  int dt;
+  if (!type_of(dtype, dt) || rows < 1 || classes < 1 || classes > MAX_CLASSES || top < 0 || top > TOP_MAX) return 0;
+  return logits_workspace_bytes(dt, rows, classes, top);
+}
+
+hpf_status hpf_op_logprob_forward(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* labels, float* logprob,
+                                  float* entropy, int32_t* rank, float* stats, int32_t* top_index, float* top_logprob, int32_t top,
+                                  int32_t rows, int32_t classes, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int dt;
+  hpf_status st = logits_shape(dtype, logits, ld, top, rows, classes, dt);
+  if (st != HPF_OK) return st;
+  if (rows == 0) return HPF_OK;
+  if (top && (!top_index || !top_logprob)) return fail(HPF_EINVAL, "top_index and top_logprob are required with a list");
+  if ((logprob || rank) && !labels) return fail(HPF_EINVAL, "labels are required for logprob and rank");
+  st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
+  if (st != HPF_OK) return st;
+  const LogprobForward a{logits, ld, labels, logprob, entropy, rank, stats, top_index, top_logprob, top, rows, classes};
+  return launched(launch_logprob_forward(dt, a, workspace, (hipStream_t)hip_stream));
+}
+
+hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* labels, const float* stats,
+                                   const float* grad_logprob, const float* entropy, const float* grad_entropy, void* dlogits,
+                                   int64_t ldd, int32_t rows, int32_t classes, void* hip_stream) {
+  int dt;
+  hpf_status st = logits_shape(dtype, logits, ld, 0, rows, classes, dt);
+  if (st != HPF_OK) return st;
+  if (rows == 0) return HPF_OK;
+  if (!stats || !dlogits) return fail(HPF_EINVAL, "stats and dlogits are required");
+  if (grad_logprob && !labels) return fail(HPF_EINVAL, "labels are required with grad_logprob");
+  if (grad_entropy && !entropy) return fail(HPF_EINVAL, "entropy is required with grad_entropy");
+  if (!rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
+  if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
+  if (overlap(logits, span(dt, rows, classes, ld), dlogits, span(dt, rows, classes, ldd)) && (logits != dlogits || ld != ldd))
+    return fail(HPF_EINVAL, "dlogits overlap the logits (they may be the same tensor)");
+  const LogprobBackward a{logits, ld, labels, stats, grad_logprob, entropy, grad_entropy, dlogits, ldd, rows, classes};
+  return launched(launch_logprob_backward(dt, a, (hipStream_t)hip_stream));
+}
+
+hpf_status hpf_op_distill(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* top_index, const float* top_logit,
+                          int32_t top, const int32_t* labels, float temperature, float hard_weight, const float* row_weight,
+                          float* loss, void* dlogits, int64_t ldd, int32_t rows, int32_t classes, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  int dt;
+  hpf_status st = logits_shape(dtype, logits, ld, top, rows, classes, dt);
+  if (st != HPF_OK) return st;
+  if (!(temperature >= 1e-4f && temperature <= 1e4f)) return fail(HPF_EINVAL, "temperature %g outside [1e-4, 1e4]", (double)temperature);
+  if (!(hard_weight >= 0.f && hard_weight <= 1.f)) return fail(HPF_EINVAL, "hard_weight %g outside [0, 1]", (double)hard_weight);
+  if (rows == 0) return HPF_OK;
+  if (!loss) return fail(HPF_EINVAL, "null loss");
+  if (top && (!top_index || !top_logit)) return fail(HPF_EINVAL, "top_index and top_logit are required with a list");
+  if (hard_weight > 0.f && !labels) return fail(HPF_EINVAL, "labels are required with hard_weight > 0");
+  if (dlogits && !rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
+  if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
+  if (overlap(logits, span(dt, rows, classes, ld), dlogits, span(dt, rows, classes, ldd))) return fail(HPF_EINVAL, "dlogits overlap the logits");
+  st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
+  if (st != HPF_OK) return st;
+  const Distill a{logits, ld, top_index, top_logit, labels, row_weight, loss, dlogits, ldd, temperature, hard_weight, top, rows, classes};
+  return launched(launch_distill(dt, a, workspace, (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhpf.so")
@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(HERE, "libhpf.so")
 HPF_ABI_VERSION = 2
 HPF_OK, HPF_EINVAL, HPF_ESTATE, HPF_ENOMEM, HPF_EDEVICE, HPF_EUNSUPPORTED = range(6)
 HPF_F32, HPF_BF16 = 0, 1
+HPF_ACT_NONE, HPF_ACT_RELU, HPF_ACT_GELU, HPF_ACT_SILU = range(4)
+ACTIVATIONS = {"none": HPF_ACT_NONE, "relu": HPF_ACT_RELU, "gelu": HPF_ACT_GELU, "silu": HPF_ACT_SILU}
 STATUS_NAMES = {0: "HPF_OK", 1: "HPF_EINVAL", 2: "HPF_ESTATE", 3: "HPF_ENOMEM", 4: "HPF_EDEVICE",
                 5: "HPF_EUNSUPPORTED"}
 
@@ -92,6 +94,19 @@ def _load():
     L.hpf_op_bn_relu_forward.argtypes = [C.c_int, vp, vp, vp, C.c_float, vp, vp, i32, i32, vp, sz, vp]
     L.hpf_op_bn_relu_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, sz, vp]
     L.hpf_op_bn_relu_forward_noalloc.argtypes = [C.c_int, vp, vp, vp, C.c_float, vp, vp, i32, i32, vp]
+    i64 = C.c_int64
+    L.hpf_op_linear_packed_bytes.argtypes = [i32, i32]
+    L.hpf_op_linear_packed_bytes.restype = sz
+    L.hpf_op_linear_pack.argtypes = [vp, i32, i32, vp, sz, vp]
+    L.hpf_op_linear_workspace_bytes.argtypes = [C.c_int, i32, i32, i32]
+    L.hpf_op_linear_workspace_bytes.restype = sz
+    L.hpf_op_linear_forward.argtypes = [C.c_int, vp, i64, vp, vp, vp, i64, vp, i64, vp, i32, i32, i32, i32, vp, sz, vp]
+    L.hpf_op_linear_backward.argtypes = [C.c_int, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, i32, i32, i32, i32, vp, sz, vp]
+    L.hpf_op_logits_workspace_bytes.argtypes = [C.c_int, i32, i32, i32]
+    L.hpf_op_logits_workspace_bytes.restype = sz
+    L.hpf_op_logprob_forward.argtypes = [C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, sz, vp]
+    L.hpf_op_logprob_backward.argtypes = [C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, i64, i32, i32, vp]
+    L.hpf_op_distill.argtypes = [C.c_int, vp, i64, vp, vp, i32, vp, C.c_float, C.c_float, vp, vp, vp, i64, i32, i32, vp, sz, vp]
     L.hpf_partition_check.argtypes = [vp]
     L.hpf_debug_set_invalid.argtypes = [vp, i32]
     L.hpf_stash_read.argtypes = [vp, i32, i32, i32, vp, sz, C.POINTER(sz), C.POINTER(i32)]
@@ -111,7 +126,10 @@ EXPORTS = ["hpf_partition_sizes", "hpf_partition_create", "hpf_forward_microbatc
            "hpf_bn_running_read", "hpf_bn_running_write", "hpf_forward_inference", "hpf_forward_inference_group",
            "hpf_last_error", "hpf_op_workspace_bytes", "hpf_op_conv_forward",
            "hpf_op_conv_dgrad", "hpf_op_conv_wgrad", "hpf_op_bn_relu_forward", "hpf_op_bn_relu_backward",
-           "hpf_stash_read", "hpf_partition_check", "hpf_debug_set_invalid", "hpf_op_bn_relu_forward_noalloc", "hpf_probe_copy", "hpf_probe_mfma_bf16"]
+           "hpf_stash_read", "hpf_partition_check", "hpf_debug_set_invalid", "hpf_op_bn_relu_forward_noalloc",
+           "hpf_op_linear_packed_bytes", "hpf_op_linear_pack", "hpf_op_linear_workspace_bytes", "hpf_op_linear_forward",
+           "hpf_op_linear_backward", "hpf_op_logits_workspace_bytes", "hpf_op_logprob_forward", "hpf_op_logprob_backward",
+           "hpf_op_distill", "hpf_probe_copy", "hpf_probe_mfma_bf16"]
 
 
 def hpf_last_error() -> str:
@@ -314,6 +332,71 @@ def hpf_op_bn_relu_forward_noalloc(dtype, x, gamma, beta, eps, a, stats, M, Cc, 
     _check(lib.hpf_op_bn_relu_forward_noalloc(dtype, x, gamma, beta, eps, a, stats, M, Cc, stream))
 
 
+def hpf_op_linear_packed_bytes(K, N) -> int:
+    return int(lib.hpf_op_linear_packed_bytes(K, N))
+
+
+def hpf_op_linear_pack(w, K, N, packed, packed_bytes, stream=0):
+    _check(lib.hpf_op_linear_pack(w, K, N, packed, packed_bytes, stream or None))
+
+
+def hpf_op_linear_workspace_bytes(dtype, M, K, N) -> int:
+    return int(lib.hpf_op_linear_workspace_bytes(dtype, M, K, N))
+
+
+def hpf_op_linear_forward(dtype, x, ldx, weights, bias, residual, ldr, y, ldy, slope, M, K, N, activation, workspace=0,
+                          workspace_bytes=0, stream=0):
+    _check(lib.hpf_op_linear_forward(dtype, x, ldx, weights, bias, residual, ldr, y, ldy, slope, M, K, N, activation, workspace,
+                                     workspace_bytes, stream))
+
+
+def hpf_op_linear_backward(dtype, dy, lddy, x, ldx, weights, slope, dx, lddx, dw, db, accumulate, M, K, N, workspace=0,
+                           workspace_bytes=0, stream=0):
+    _check(lib.hpf_op_linear_backward(dtype, dy, lddy, x, ldx, weights, slope, dx, lddx, dw, db, int(accumulate), M, K, N,
+                                      workspace, workspace_bytes, stream))
+
+
+def hpf_op_logits_workspace_bytes(dtype, rows, classes, top) -> int:
+    return int(lib.hpf_op_logits_workspace_bytes(dtype, rows, classes, top))
+
+
+def hpf_op_logprob_forward(dtype, logits, ld, labels, logprob, entropy, rank, stats, top_index, top_logprob, top, rows, classes,
+                           workspace=0, workspace_bytes=0, stream=0):
+    _check(lib.hpf_op_logprob_forward(dtype, logits, ld, labels, logprob, entropy, rank, stats, top_index, top_logprob, top, rows,
+                                      classes, workspace, workspace_bytes, stream))
+
+
+def hpf_op_logprob_backward(dtype, logits, ld, labels, stats, grad_logprob, entropy, grad_entropy, dlogits, ldd, rows, classes,
+                            stream=0):
+    _check(lib.hpf_op_logprob_backward(dtype, logits, ld, labels, stats, grad_logprob, entropy, grad_entropy, dlogits, ldd, rows,
+                                       classes, stream))
+
+
+def hpf_op_distill(dtype, logits, ld, top_index, top_logit, top, labels, temperature, hard_weight, row_weight, loss, dlogits, ldd,
+                   rows, classes, workspace=0, workspace_bytes=0, stream=0):
+    _check(lib.hpf_op_distill(dtype, logits, ld, top_index, top_logit, top, labels, temperature, hard_weight, row_weight, loss,
+                              dlogits, ldd, rows, classes, workspace, workspace_bytes, stream))
+
+
+class LinearWeights:
+    """Weights of a product as `Ops.linear_forward` / `linear_backward` take them: the fp32 master w [K, N] in the check mode,
+    its two bf16 layouts otherwise.  After a change of w: `Ops.linear_weights(w, out=weights)`."""
+    __slots__ = ("K", "N", "dtype", "tensor", "ptr")
+
+    def __init__(self, K, N, dtype, tensor, ptr):
+        self.K, self.N, self.dtype, self.tensor, self.ptr = K, N, dtype, tensor, ptr
+
+
+class LogProb(NamedTuple):
+    """Per row of logits: what `Ops.logprob_forward` gives."""
+    logprob: "Optional[torch.Tensor]"        # of the label
+    entropy: "torch.Tensor"
+    rank: "Optional[torch.Tensor]"           # of the label: classes in front of it
+    stats: "torch.Tensor"                    # for logprob_backward
+    top_index: "Optional[torch.Tensor]"
+    top_logprob: "Optional[torch.Tensor]"
+
+
 def hpf_probe_copy(dst, src, nbytes, stream=0):
     _check(lib.hpf_probe_copy(dst, src, nbytes, stream))
 
@@ -393,6 +476,166 @@ class Ops:
                                 skip.data_ptr() if skip is not None else 0, dx.data_ptr(), dg.data_ptr(), db.data_ptr(),
                                 M, Cc, ws, n, self._s())
         return dx, dg, db
+
+    # ---- the answer end of a model.  Tensors are of this object's type (rows may have a stride), on its device; work goes to
+    # the device's current stream, workspaces come from torch's allocator of that stream.
+    def _here(self, t):
+        return t.device == self.device or (self.device.index is None and t.device.type == self.device.type
+                                           and t.device.index == self.torch.cuda.current_device())
+
+    def _rows(self, name, t, shape=None, dtype=None):
+        """(address, row stride) of a matrix; raises ValueError for what the library could not tell from an address."""
+        if t is None:
+            return 0, 0
+        if t.dtype != (dtype or self.tdtype):
+            raise ValueError(f"{name}: expected {dtype or self.tdtype}, got {t.dtype}")
+        if not self._here(t):
+            raise ValueError(f"{name}: on {t.device}, expected {self.device}")
+        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape or '[rows, columns]'}")
+        rows, cols = t.shape
+        ld = t.stride(0) if rows > 1 else max(cols, 1)
+        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+            raise ValueError(f"{name}: strides {t.stride()}: columns must be contiguous and rows must not overlap")
+        return t.data_ptr(), ld
+
+    def _dense(self, name, t, shape, dtype):
+        if t is None:
+            return 0
+        if t.dtype != dtype or not self._here(t) or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _scratch(self, n):
+        """(tensor to keep alive until the call is enqueued, address)"""
+        if not n:
+            return None, 0
+        t = self.torch.empty(n + 256, dtype=self.torch.uint8, device=self.device)
+        return t, (t.data_ptr() + 255) // 256 * 256
+
+    def linear_weights(self, w, out=None):
+        """w: fp32 [K, N].  out: the object of an earlier call, which gets the new weights in place."""
+        torch = self.torch
+        K, N = w.shape
+        ptr = self._dense("w", w, (K, N), torch.float32)
+        if out is not None and (out.K, out.N, out.dtype) != (K, N, self.dt):
+            raise ValueError("out: weights of another shape or type")
+        if self.dt == HPF_F32:
+            if out is None:
+                return LinearWeights(K, N, self.dt, w, ptr)
+            out.tensor, out.ptr = w, ptr
+            return out
+        n = hpf_op_linear_packed_bytes(K, N)
+        if out is None:
+            t, at = self._scratch(n)
+            out = LinearWeights(K, N, self.dt, t, at)
+        with torch.cuda.device(self.device):
+            hpf_op_linear_pack(ptr, K, N, out.ptr, n, self._s())
+        return out
+
+    def _weights(self, weights):
+        if weights.dtype != self.dt or not self._here(weights.tensor):
+            raise ValueError("weights: laid out for another type or device")
+        return weights.K, weights.N, weights.ptr
+
+    def linear_forward(self, x, weights, bias=None, residual=None, activation="none", slope=False, out=None):
+        """y = act(x w + bias) + residual; with slope=True (y, act'(x w + bias)), the second None without activation."""
+        torch = self.torch
+        K, N, wp = self._weights(weights)
+        xp, ldx = self._rows("x", x)
+        M = x.shape[0]
+        if x.shape[1] != K:
+            raise ValueError(f"x: {x.shape[1]} columns, the weights have {K} rows")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
+        bp = self._dense("bias", bias, (N,), torch.float32)
+        rp, ldr = self._rows("residual", residual, (M, N))
+        y = out if out is not None else torch.empty((M, N), dtype=self.tdtype, device=self.device)
+        yp, ldy = self._rows("out", y, (M, N))
+        sl = torch.empty((M, N), dtype=self.tdtype, device=self.device) if slope and activation != "none" else None
+        with torch.cuda.device(self.device):
+            n = hpf_op_linear_workspace_bytes(self.dt, M, K, N)
+            ws, wsp = self._scratch(n)
+            hpf_op_linear_forward(self.dt, xp, ldx, wp, bp, rp, ldr, yp, ldy, sl.data_ptr() if sl is not None else 0, M, K, N,
+                                  ACTIVATIONS[activation], wsp, n, self._s())
+        return (y, sl) if slope else y
+
+    def linear_backward(self, dy, x, weights, slope=None, need_dx=True, dw=None, db=None, accumulate=False):
+        """(dx, dw, db) from the gradient of y; dw [K, N] and db [N] are fp32, added to if accumulate (then required)."""
+        torch = self.torch
+        K, N, wp = self._weights(weights)
+        dyp, lddy = self._rows("dy", dy)
+        M = dy.shape[0]
+        if dy.shape[1] != N:
+            raise ValueError(f"dy: {dy.shape[1]} columns, the weights have {N}")
+        xp, ldx = self._rows("x", x, (M, K))
+        sp = self._dense("slope", slope, (M, N), self.tdtype)
+        if accumulate and (dw is None or db is None):
+            raise ValueError("accumulate: dw and db are required")
+        dx = torch.empty((M, K), dtype=self.tdtype, device=self.device) if need_dx else None
+        dw = torch.empty((K, N), dtype=torch.float32, device=self.device) if dw is None else dw
+        db = torch.empty(N, dtype=torch.float32, device=self.device) if db is None else db
+        dwp, dbp = self._dense("dw", dw, (K, N), torch.float32), self._dense("db", db, (N,), torch.float32)
+        with torch.cuda.device(self.device):
+            n = hpf_op_linear_workspace_bytes(self.dt, M, K, N)
+            ws, wsp = self._scratch(n)
+            hpf_op_linear_backward(self.dt, dyp, lddy, xp, ldx, wp, sp, dx.data_ptr() if need_dx else 0, K, dwp, dbp, accumulate,
+                                   M, K, N, wsp, n, self._s())
+        return dx, dw, db
+
+    def _labels(self, labels, rows):
+        return self._dense("labels", labels, (rows,), self.torch.int32)
+
+    def logprob_forward(self, logits, labels=None, top=0):
+        """Log probability and rank of the labels, entropy and the `top` most likely classes of every row: a LogProb."""
+        torch = self.torch
+        lp, ld = self._rows("logits", logits)
+        rows, classes = logits.shape
+        lab = self._labels(labels, rows)
+
+        def new(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        r = LogProb(new(rows) if labels is not None else None, new(rows), new(rows, dtype=torch.int32) if labels is not None else None,
+                    new(rows, 2), new(rows, top, dtype=torch.int32) if top > 0 else None, new(rows, top) if top > 0 else None)
+        with torch.cuda.device(self.device):
+            n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
+            ws, wsp = self._scratch(n)
+            p = [t.data_ptr() if t is not None else 0 for t in r]
+            hpf_op_logprob_forward(self.dt, lp, ld, lab, p[0], p[1], p[2], p[3], p[4], p[5], top, rows, classes, wsp, n, self._s())
+        return r
+
+    def logprob_backward(self, logits, labels, stats, grad_logprob=None, entropy=None, grad_entropy=None, out=None):
+        """Gradient of log probability and entropy with respect to the logits; out may be the logits."""
+        torch = self.torch
+        lp, ld = self._rows("logits", logits)
+        rows, classes = logits.shape
+        f32 = torch.float32
+        d = out if out is not None else torch.empty((rows, classes), dtype=self.tdtype, device=self.device)
+        dp, ldd = self._rows("out", d, (rows, classes))
+        with torch.cuda.device(self.device):
+            hpf_op_logprob_backward(self.dt, lp, ld, self._labels(labels, rows), self._dense("stats", stats, (rows, 2), f32),
+                                    self._dense("grad_logprob", grad_logprob, (rows,), f32), self._dense("entropy", entropy, (rows,), f32),
+                                    self._dense("grad_entropy", grad_entropy, (rows,), f32), dp, ldd, rows, classes, self._s())
+        return d
+
+    def distill(self, logits, top_index, top_logit, labels=None, temperature=1.0, hard_weight=0.0, row_weight=None, gradient=True):
+        """(loss per row, dlogits) of a student against the teacher's list [rows, top] and the hard label; dlogits is None
+        without gradient."""
+        torch = self.torch
+        lp, ld = self._rows("logits", logits)
+        rows, classes = logits.shape
+        top = top_index.shape[1] if top_index is not None else 0
+        ti = self._dense("top_index", top_index, (rows, top), torch.int32)
+        tl = self._dense("top_logit", top_logit, (rows, top), torch.float32)
+        loss = torch.empty(rows, dtype=torch.float32, device=self.device)
+        d = torch.empty((rows, classes), dtype=self.tdtype, device=self.device) if gradient else None
+        with torch.cuda.device(self.device):
+            n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
+            ws, wsp = self._scratch(n)
+            hpf_op_distill(self.dt, lp, ld, ti, tl, top, self._labels(labels, rows), temperature, hard_weight,
+                           self._dense("row_weight", row_weight, (rows,), torch.float32), loss.data_ptr(),
+                           d.data_ptr() if gradient else 0, classes, rows, classes, wsp, n, self._s())
+        return loss, d
 
 
 class Partition:
