@@ -131,6 +131,298 @@ __global__ __launch_bounds__(256) void k_linear_tile(Operand<T> A, Operand<T> B,
       }
 }
 
+// ---- bf16: tiles on matrix cores -------------------------------------------------------------------------------------
+// C[m][n] = sum_k A[m][k] B[n][k], both operands with k contiguous, rows on 16 bytes; k >= K counts as 0 in A, and B's rows are padded
+// with zeros to a multiple of 64.
+enum : int { OUT_Y = 0, OUT_SUM = 1, OUT_SLAB = 2 };
+struct Product {
+  const bf16_t* A; long lda;
+  const bf16_t* B; long ldb;
+  int M, N, K;
+  // OUT_Y
+  const float* bias;
+  const bf16_t* residual; long ldr;
+  bf16_t* y; long ldy;
+  bf16_t* slope;
+  int act;
+  // OUT_SUM: C in fp32 [M][N]; OUT_SLAB: this share's C, [splits][M][N]
+  float* sum; int accumulate;
+};
+
+__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};   // where lanes beyond the end of a row read
+
+// Phi(z) and the normal density by one exponential: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26
+// (absolute error of erfc 1.5e-7, a hundredth of a bf16 step at 1)
+__device__ __forceinline__ void normal(float z, float& below, float& density) {
+  const float x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f)), e = __expf(-x * x);
+  const float q = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  below = z < 0.f ? q : 1.f - q;
+  density = 0.39894228f * e;
+}
+__device__ __forceinline__ void activate_fast(int act, float z, float& y, float& slope) {
+  if (act == ACT_GELU) {
+    float below, density;
+    normal(z, below, density);
+    y = z * below;
+    slope = fmaf(z, density, below);
+  } else if (act == ACT_SILU) {
+    const float q = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    y = z * q;
+    slope = q * fmaf(z, 1.f - q, 1.f);
+  } else {
+    activate<float>(act, z, y, slope);
+  }
+}
+
+// eight consecutive results of a row, n a multiple of 8
+template <int OUT>
+__device__ __forceinline__ void finish8(const Product& p, int m, int n, float (&v)[8], unsigned split) {
+  const int left = p.N - n;
+  if (OUT != OUT_Y) {
+    float* o = p.sum + ((size_t)(OUT == OUT_SLAB ? split : 0) * p.M + m) * p.N + n;
+    const bool add = OUT == OUT_SUM && p.accumulate;
+    if (left >= 8 && (p.N & 3) == 0) {
+      if (add) {
+        float w[8];
+        load8(o, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += w[e];
+      }
+      store8(o, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) o[e] = add ? o[e] + v[e] : v[e];
+    }
+    return;
+  }
+  const bool whole = left >= 8;
+  if (p.bias) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += p.bias[n + (e < left ? e : 0)];
+  }
+  float sl[8], r[8];
+  if (p.act != ACT_NONE) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float y;
+      activate_fast(p.act, v[e], y, sl[e]);
+      v[e] = y;
+    }
+    if (p.slope) {
+      bf16_t* o = p.slope + (size_t)m * p.N + n;
+      if (whole && (p.N & 7) == 0 && ((uintptr_t)p.slope & 15) == 0) store8(o, sl);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < left) o[e] = f32_to_bf16(sl[e]);
+    }
+  } else if (p.slope) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p.slope[(size_t)m * p.N + n + e] = f32_to_bf16(1.f);
+  }
+  if (p.residual) {
+    const bf16_t* o = p.residual + m * p.ldr + n;
+    if (whole && (p.ldr & 7) == 0 && ((uintptr_t)p.residual & 15) == 0) load8(o, r);
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = e < left ? bf16_to_f32(o[e]) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += r[e];
+  }
+  bf16_t* o = p.y + m * p.ldy + n;
+  if (whole && (p.ldy & 7) == 0 && ((uintptr_t)p.y & 15) == 0) store8(o, v);
+  else
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) o[e] = f32_to_bf16(v[e]);
+}
+
+// Work-group i of n: the die it runs on is i % 8 (each has its own L2), so die d takes the d-th eighth of the tiles, and neighbours in that
+// order share operands: blocks of GROUP tile rows, column by column.
+__device__ __forceinline__ void tile_of(unsigned i, unsigned rows, unsigned cols, unsigned& r, unsigned& c) {
+  constexpr unsigned GROUP = 8;
+  const unsigned n = rows * cols, die = i & 7, at = i >> 3, share = n >> 3, extra = n & 7;
+  const unsigned t = die * share + (die < extra ? die : extra) + at;
+  const unsigned g = t / (GROUP * cols), r0 = g * GROUP, h = rows - r0 < GROUP ? rows - r0 : GROUP, u = t - g * GROUP * cols;
+  c = u / h;
+  r = r0 + (u - c * h);
+}
+
+// BM x BN tile by WM x WN waves; 64 of the contraction per step, two stages in LDS, loaded past the registers.  A stage's row is 128 bytes;
+// its 16-byte units are stored in the order unit ^ (row & 7), so that 8 neighbouring rows' reads of one unit fall on all banks.
+template <int BM, int BN, int WM, int WN, int OUT>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigned tile_rows, unsigned tile_cols, int steps_per_split) {
+  constexpr int NT = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * 64;
+  constexpr int LA = BM * 8 / NT, LB = BN * 8 / NT;      // 16-byte units per thread and step
+  extern __shared__ __align__(16) bf16_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave / WN, wn = wave % WN;
+  unsigned tr, tc;
+  tile_of(blockIdx.x, tile_rows, tile_cols, tr, tc);
+  const int m0 = (int)tr * BM, n0 = (int)tc * BN;
+  const int k_begin = (int)blockIdx.y * steps_per_split, k_all = (p.K + 63) / 64;
+  const int steps = (k_all - k_begin < steps_per_split ? k_all - k_begin : steps_per_split);
+
+  // thread: rows tid / 8 + i * NT / 8, unit tid % 8 of the stage, which holds unit (tid ^ row) % 8 of the operand
+  const int unit = (tid ^ (tid >> 3)) & 7;
+  const bf16_t* pa[LA];
+  const bf16_t* pb[LB];
+#pragma unroll
+  for (int i = 0; i < LA; ++i) {
+    const int r = m0 + (tid >> 3) + i * (NT / 8);
+    pa[i] = p.A + (r < p.M ? r : p.M - 1) * p.lda + k_begin * 64 + unit * 8;
+  }
+#pragma unroll
+  for (int i = 0; i < LB; ++i) {
+    const int r = n0 + (tid >> 3) + i * (NT / 8);
+    pb[i] = p.B + (r < p.N ? r : p.N - 1) * p.ldb + k_begin * 64 + unit * 8;
+  }
+  const int k_left = p.K - k_begin * 64 - unit * 8;      // > 0: the unit of step 0 is there
+  auto load = [&](int step, int st) {
+    bf16_t* s = smem + st * STAGE + wave * 512;
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+      const bf16_t* g = k_left > step * 64 ? pa[i] + step * 64 : (const bf16_t*)kZeros;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, (__attribute__((address_space(3))) void*)(s + i * (NT * 8)), 16, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pb[i] + step * 64),
+                                       (__attribute__((address_space(3))) void*)(s + BM * 64 + i * (NT * 8)), 16, 0, 0);
+  };
+
+  floatx4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  const int row = lane & 15, q = lane >> 4;
+  const int at_a = (wm * (BM / WM) + row) * 64, at_b = BM * 64 + (wn * (BN / WN) + row) * 64;
+  const int u0 = ((q) ^ (row & 7)) * 8, u1 = ((q + 4) ^ (row & 7)) * 8;
+  load(0, 0);
+  for (int t = 0; t < steps; ++t) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): this step's units are in LDS
+    __syncthreads();
+    if (t + 1 < steps) load(t + 1, (t + 1) & 1);
+    const bf16_t* s = smem + (t & 1) * STAGE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int u = h ? u1 : u0;
+      bf16x8 a[TM], b[TN];
+#pragma unroll
+      for (int i = 0; i < TN; ++i) b[i] = *reinterpret_cast<const bf16x8*>(s + at_b + i * 1024 + u);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) a[j] = *reinterpret_cast<const bf16x8*>(s + at_a + j * 1024 + u);
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int i = 0; i < TN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[i], a[j], acc[i][j], 0, 0, 0);
+    }
+  }
+  __syncthreads();
+
+  // A wave's results go through its own part of LDS, 16 rows at a time, so that a lane ends up with 8 consecutive columns
+  constexpr int TS = BN / WN + 4;                        // fp32 row stride: rows shift by 4 banks
+  constexpr int LANES = BN / WN / 8, ROWS = 64 / LANES;  // lanes per row, rows per pass
+  static_assert(16 * TS * 4 * WM * WN <= 2 * STAGE * 2, "the rows of all waves fit the stages");
+  float* mine = reinterpret_cast<float*>(smem) + wave * 16 * TS;
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+#pragma unroll
+    for (int i = 0; i < TN; ++i) *reinterpret_cast<floatx4*>(mine + row * TS + i * 16 + q * 4) = acc[i][j];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = 0; r < 16; r += ROWS) {
+      const int rl = r + lane / LANES, m = m0 + wm * (BM / WM) + j * 16 + rl, n = n0 + wn * (BN / WN) + (lane % LANES) * 8;
+      float v[8];
+      load8(mine + rl * TS + (lane % LANES) * 8, v);
+      if (m < p.M && n < p.N) finish8<OUT>(p, m, n, v, blockIdx.y);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// y or the sum from the shares of a split contraction
+template <int OUT>
+__global__ __launch_bounds__(256) void k_linear_join(Product p, const float* __restrict__ slabs, int splits) {
+  const int units = (p.N + 7) / 8;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)p.M * units; i += (size_t)gridDim.x * 256) {
+    const int m = (int)(i / units), n = (int)(i - (size_t)m * units) * 8, left = p.N - n;
+    float v[8] = {};
+    for (int s = 0; s < splits; ++s) {
+      const float* o = slabs + ((size_t)s * p.M + m) * p.N + n;
+      float w[8];
+      if (left >= 8 && (p.N & 3) == 0) load8(o, w);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = e < left ? o[e] : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
+    finish8<OUT>(p, m, n, v, 0);
+  }
+}
+
+// Rows that do not start on 16 bytes or are no multiple of 8 long: copied to [M][ld], zeros behind the end
+__global__ __launch_bounds__(256) void k_linear_rows(const bf16_t* __restrict__ src, long lds, bf16_t* __restrict__ dst, int ld, int M, int K) {
+  const int units = ld / 8;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)M * units; i += (size_t)gridDim.x * 256) {
+    const int m = (int)(i / units), k = (int)(i - (size_t)m * units) * 8;
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + e < K) w[e >> 1] |= (uint32_t)src[m * lds + k + e] << (16 * (e & 1));
+    *reinterpret_cast<uint4*>(dst + (size_t)m * ld + k) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// Transposed copy dst[c][m] of src[m][c] (* slope), columns c < cols, m padded to ld with zeros; with rows: also the product itself to
+// rows[m][rld] (c padded to rld with zeros), and with sums: the column sums of each 64 rows.  64 x 64 per work-group.
+__global__ __launch_bounds__(256) void k_linear_turn(const bf16_t* __restrict__ src, long lds, const bf16_t* __restrict__ slope,
+                                                     bf16_t* __restrict__ dst, int ld, bf16_t* __restrict__ rows, int rld,
+                                                     float* __restrict__ sums, int M, int cols) {
+  __shared__ bf16_t tile[64][66];
+  const int m0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x;
+  for (int i = tid; i < 64 * 64; i += 256) {
+    const int m = m0 + i / 64, c = c0 + i % 64;
+    bf16_t v = 0;
+    if (m < M && c < cols) {
+      v = src[m * lds + c];
+      if (slope) v = f32_to_bf16(bf16_to_f32(v) * bf16_to_f32(slope[(size_t)m * cols + c]));
+    }
+    tile[i / 64][i % 64] = v;
+    if (rows && m < M && c < rld) rows[(size_t)m * rld + c] = v;
+  }
+  __syncthreads();
+  if (dst)
+    for (int i = tid; i < 64 * 64; i += 256) {
+      const int c = c0 + i / 64, m = m0 + i % 64;
+      if (c < cols && m < ld) dst[(size_t)c * ld + m] = tile[i % 64][i / 64];
+    }
+  if (sums && tid < 64 && c0 + tid < cols) {
+    float s = 0.f;
+    for (int m = 0; m < 64; ++m) s += bf16_to_f32(tile[m][tid]);
+    sums[(size_t)blockIdx.y * cols + c0 + tid] = s;
+  }
+}
+// db from the sums of all groups of 64 rows, one order
+__global__ __launch_bounds__(256) void k_linear_db_join(const float* __restrict__ sums, int groups, float* __restrict__ db, int accumulate, int N) {
+  __shared__ float part[4][64];
+  const int c = threadIdx.x & 63, g = threadIdx.x >> 6, n = blockIdx.x * 64 + c;
+  float s = 0.f;
+  if (n < N)
+    for (int i = g; i < groups; i += 4) s += sums[(size_t)i * N + n];
+  part[g][c] = s;
+  __syncthreads();
+  if (g == 0 && n < N) {
+    s = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+    db[n] = accumulate ? s + db[n] : s;
+  }
+}
+
 // packed copies of w: blocks of 64 x 64 through LDS
 __global__ __launch_bounds__(256) void k_linear_pack(const float* __restrict__ w, bf16_t* __restrict__ packed, int K, int N, int Kp, int Np) {
   __shared__ float tile[64][65];
@@ -175,50 +467,167 @@ __global__ __launch_bounds__(256) void k_linear_db(const T* __restrict__ dz, lon
 }
 
 unsigned blocks64(int v) { return (unsigned)((v + 63) / 64); }
+unsigned grid_for(size_t n, size_t per, size_t cap) {
+  const size_t g = (n + per - 1) / per;
+  return (unsigned)(g < 1 ? 1 : g > cap ? cap : g);
+}
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-template <class T>
-hipError_t tile(const Operand<T>& A, const Operand<T>& B, const Epilogue<T>& e, int M, int N, int K, hipStream_t s) {
-  k_linear_tile<T><<<dim3(blocks64(N), blocks64(M)), 256, 0, s>>>(A, B, e, M, N, K);
+// How a bf16 product is cut
+struct Cut {
+  bool large;
+  int splits, steps;            // steps of 64 per share
+  unsigned rows, cols;          // tiles
+};
+Cut cut_of(int M, int N, int K) {
+  Cut c;
+  const long big = (long)((M + 255) / 256) * ((N + 255) / 256);
+  c.large = big >= 192;
+  const int T = c.large ? 256 : 128;
+  c.rows = (unsigned)((M + T - 1) / T);
+  c.cols = (unsigned)((N + T - 1) / T);
+  const int k = (K + 63) / 64;
+  long want = c.large ? 1 : 512 / ((long)c.rows * c.cols);
+  if (want > k / 4) want = k / 4;
+  if (want < 1) want = 1;
+  c.steps = (int)((k + want - 1) / want);
+  c.splits = (k + c.steps - 1) / c.steps;
+  return c;
+}
+size_t slab_bytes(int M, int N, int K) {
+  const Cut c = cut_of(M, N, K);
+  return c.splits > 1 ? align256((size_t)c.splits * M * N * sizeof(float)) : 0;
+}
+
+template <int BM, int BN, int WM, int WN, int OUT>
+hipError_t mfma(const Product& p, const Cut& c, hipStream_t s) {
+  constexpr int lds = 2 * (BM + BN) * 64 * 2;
+  const auto kernel = k_linear_mfma<BM, BN, WM, WN, OUT>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3(c.rows * c.cols, (unsigned)c.splits), 64 * WM * WN, lds, s>>>(p, c.rows, c.cols, c.steps);
   return hipGetLastError();
 }
 
-// The weights as operands: rows n for the forward product, rows k for dx
-Operand<bf16_t> forward_operand(const void* p, int K, int, bf16_t) { return {(const bf16_t*)p, round_up64(K), 1}; }
-Operand<float> forward_operand(const void* p, int, int N, float) { return {(const float*)p, 1, N}; }
-Operand<bf16_t> dx_operand(const void* p, int K, int N, bf16_t) { return {(const bf16_t*)p + (size_t)N * round_up64(K), round_up64(N), 1}; }
-Operand<float> dx_operand(const void* p, int, int N, float) { return {(const float*)p, N, 1}; }
-
-template <class T>
-hipError_t forward(const LinearForward& a, hipStream_t s) {
-  Epilogue<T> e{a.bias, (const T*)a.residual, a.ldr, (T*)a.y, a.ldy, (T*)a.slope, nullptr, 0, a.act};
-  return tile<T>({(const T*)a.x, a.ldx, 1}, forward_operand(a.weights, a.K, a.N, T{}), e, a.M, a.N, a.K, s);
+// OUT: OUT_Y or OUT_SUM; slabs: room for slab_bytes
+template <int OUT>
+hipError_t product(const Product& p, float* slabs, hipStream_t s) {
+  const Cut c = cut_of(p.M, p.N, p.K);
+  if (c.large) return mfma<256, 256, 2, 4, OUT>(p, c, s);
+  if (c.splits == 1) return mfma<128, 128, 2, 2, OUT>(p, c, s);
+  Product q = p;
+  q.sum = slabs;
+  const hipError_t e = mfma<128, 128, 2, 2, OUT_SLAB>(q, c, s);
+  if (e != hipSuccess) return e;
+  k_linear_join<OUT><<<grid_for((size_t)p.M * ((p.N + 7) / 8), 256, 2048), 256, 0, s>>>(p, slabs, c.splits);
+  return hipGetLastError();
 }
 
-template <class T>
-hipError_t backward(const LinearBackward& a, void* workspace, hipStream_t s) {
-  const T* dz = (const T*)a.dy;
+bool direct(const void* p, long ld, int K) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (K & 7) == 0; }
+
+hipError_t forward_bf16(const LinearForward& a, char* ws, hipStream_t s) {
+  Product p{};
+  p.A = (const bf16_t*)a.x; p.lda = a.ldx; p.M = a.M; p.N = a.N; p.K = a.K;
+  if (!direct(a.x, a.ldx, a.K)) {
+    const int ld = round_up64(a.K);
+    k_linear_rows<<<grid_for((size_t)a.M * ld / 8, 256, 4096), 256, 0, s>>>((const bf16_t*)a.x, a.ldx, (bf16_t*)ws, ld, a.M, a.K);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    p.A = (const bf16_t*)ws; p.lda = ld; p.K = ld;
+  }
+  ws += align256((size_t)a.M * round_up64(a.K) * 2);
+  p.B = (const bf16_t*)a.weights; p.ldb = round_up64(a.K);
+  p.bias = a.bias; p.residual = (const bf16_t*)a.residual; p.ldr = a.ldr; p.y = (bf16_t*)a.y; p.ldy = a.ldy; p.slope = (bf16_t*)a.slope; p.act = a.act;
+  return product<OUT_Y>(p, (float*)ws, s);
+}
+
+// Workspace of a backward call: dz [M][Np] | dz^T [N][Mp] | x^T [K][Mp] | sums of 64 rows [M/64][N] | shares of a split product
+struct BackwardSpace {
+  size_t dz, dzt, xt, sums, slabs, bytes;
+  BackwardSpace(int M, int K, int N) {
+    const size_t Mp = round_up64(M), Np = round_up64(N);
+    dz = 0;
+    dzt = align256((size_t)M * Np * 2);
+    xt = dzt + align256((size_t)N * Mp * 2);
+    sums = xt + align256((size_t)K * Mp * 2);
+    slabs = sums + align256(Mp / 64 * N * 4);
+    const size_t d = slab_bytes(M, K, (int)Np), w = slab_bytes(K, N, (int)Mp);
+    bytes = slabs + (d > w ? d : w);
+  }
+};
+
+hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
+  const BackwardSpace at(a.M, a.K, a.N);
+  const int Mp = round_up64(a.M), Np = round_up64(a.N);
+  const bool copy = a.dx && (a.slope || !direct(a.dy, a.lddy, a.N));
+  bf16_t* dzt = a.dw ? (bf16_t*)(ws + at.dzt) : nullptr;
+  float* sums = a.db ? (float*)(ws + at.sums) : nullptr;
+  hipError_t e = hipSuccess;
+  if (copy || a.dw || a.db) {
+    k_linear_turn<<<dim3((unsigned)(Np / 64), (unsigned)(Mp / 64)), 256, 0, s>>>((const bf16_t*)a.dy, a.lddy, (const bf16_t*)a.slope, dzt, Mp,
+                                                                               copy ? (bf16_t*)(ws + at.dz) : nullptr, Np, sums, a.M, a.N);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && a.db) {
+    k_linear_db_join<<<blocks64(a.N), 256, 0, s>>>(sums, Mp / 64, a.db, a.accumulate, a.N);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && a.dx) {
+    Product p{};
+    p.A = copy ? (const bf16_t*)(ws + at.dz) : (const bf16_t*)a.dy; p.lda = copy ? Np : a.lddy;
+    p.B = (const bf16_t*)a.weights + (size_t)a.N * round_up64(a.K); p.ldb = Np;
+    p.M = a.M; p.N = a.K; p.K = copy ? Np : a.N;
+    p.y = (bf16_t*)a.dx; p.ldy = a.lddx;
+    e = product<OUT_Y>(p, (float*)(ws + at.slabs), s);
+  }
+  if (e == hipSuccess && a.dw) {
+    bf16_t* xt = (bf16_t*)(ws + at.xt);
+    k_linear_turn<<<dim3(blocks64(a.K), (unsigned)(Mp / 64)), 256, 0, s>>>((const bf16_t*)a.x, a.ldx, nullptr, xt, Mp, nullptr, 0, nullptr, a.M, a.K);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    Product p{};
+    p.A = xt; p.lda = Mp; p.B = dzt; p.ldb = Mp; p.M = a.K; p.N = a.N; p.K = Mp; p.sum = a.dw; p.accumulate = a.accumulate;
+    e = product<OUT_SUM>(p, (float*)(ws + at.slabs), s);
+  }
+  return e;
+}
+
+// ---- fp32 (check mode) -----------------------------------------------------------------------------------------------
+hipError_t tile(const Operand<float>& A, const Operand<float>& B, const Epilogue<float>& e, int M, int N, int K, hipStream_t s) {
+  k_linear_tile<float><<<dim3(blocks64(N), blocks64(M)), 256, 0, s>>>(A, B, e, M, N, K);
+  return hipGetLastError();
+}
+
+hipError_t forward_f32(const LinearForward& a, hipStream_t s) {
+  const Epilogue<float> e{a.bias, (const float*)a.residual, a.ldr, (float*)a.y, a.ldy, (float*)a.slope, nullptr, 0, a.act};
+  return tile({(const float*)a.x, a.ldx, 1}, {(const float*)a.weights, 1, a.N}, e, a.M, a.N, a.K, s);
+}
+
+hipError_t backward_f32(const LinearBackward& a, float* ws, hipStream_t s) {
+  const float* dz = (const float*)a.dy;
   long ld = a.lddy;
   hipError_t err = hipSuccess;
   if (a.slope) {
-    const size_t blocks = ((size_t)a.M * a.N + 2047) / 2048;
-    k_linear_dz<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(dz, ld, (const T*)a.slope, (T*)workspace, a.M, a.N);
-    dz = (const T*)workspace;
+    k_linear_dz<<<grid_for((size_t)a.M * a.N, 2048, 4096), 256, 0, s>>>(dz, ld, (const float*)a.slope, ws, a.M, a.N);
+    dz = ws;
     ld = a.N;
     err = hipGetLastError();
   }
   if (err == hipSuccess && a.db) {
-    k_linear_db<T><<<blocks64(a.N), 256, 0, s>>>(dz, ld, a.db, a.accumulate, a.M, a.N);
+    k_linear_db<<<blocks64(a.N), 256, 0, s>>>(dz, ld, a.db, a.accumulate, a.M, a.N);
     err = hipGetLastError();
   }
   if (err == hipSuccess && a.dx) {
-    Epilogue<T> e{};
-    e.y = (T*)a.dx; e.ldy = a.lddx;
-    err = tile<T>({dz, ld, 1}, dx_operand(a.weights, a.K, a.N, T{}), e, a.M, a.K, a.N, s);
+    Epilogue<float> e{};
+    e.y = (float*)a.dx; e.ldy = a.lddx;
+    err = tile({dz, ld, 1}, {(const float*)a.weights, a.N, 1}, e, a.M, a.K, a.N, s);
   }
   if (err == hipSuccess && a.dw) {
-    Epilogue<T> e{};
+    Epilogue<float> e{};
     e.sum = a.dw; e.accumulate = a.accumulate;
-    err = tile<T>({(const T*)a.x, 1, a.ldx}, {dz, 1, ld}, e, a.K, a.N, a.M, s);
+    err = tile({(const float*)a.x, 1, a.ldx}, {dz, 1, ld}, e, a.K, a.N, a.M, s);
   }
   return err;
 }
@@ -230,13 +639,17 @@ hipError_t launch_linear_pack(const float* w, bf16_t* packed, int K, int N, hipS
   return hipGetLastError();
 }
 
-size_t linear_workspace_bytes(int dt, int M, int, int N) { return (size_t)M * N * (dt == DT_BF16 ? 2 : 4); }
+size_t linear_workspace_bytes(int dt, int M, int K, int N) {
+  if (dt != DT_BF16) return (size_t)M * N * sizeof(float);
+  const size_t f = align256((size_t)M * round_up64(K) * 2) + slab_bytes(M, N, round_up64(K)), b = BackwardSpace(M, K, N).bytes;
+  return f > b ? f : b;
+}
 
-hipError_t launch_linear_forward(int dt, const LinearForward& a, void*, hipStream_t stream) {
-  return dt == DT_BF16 ? forward<bf16_t>(a, stream) : forward<float>(a, stream);
+hipError_t launch_linear_forward(int dt, const LinearForward& a, void* workspace, hipStream_t stream) {
+  return dt == DT_BF16 ? forward_bf16(a, (char*)workspace, stream) : forward_f32(a, stream);
 }
 hipError_t launch_linear_backward(int dt, const LinearBackward& a, void* workspace, hipStream_t stream) {
-  return dt == DT_BF16 ? backward<bf16_t>(a, workspace, stream) : backward<float>(a, workspace, stream);
+  return dt == DT_BF16 ? backward_bf16(a, (char*)workspace, stream) : backward_f32(a, (float*)workspace, stream);
 }
 
 }  // namespace hpf
