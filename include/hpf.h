@@ -412,7 +412,7 @@ hpf_status hpf_op_bn_relu_forward_noalloc(hpf_dtype dtype, const void* x, const 
  * (w [K][N]).  HPF_BF16: the products take bf16 copies of the weights, which hpf_op_linear_pack lays out once after every
  * change of w (2 * (N * ceil64(K) + K * ceil64(N)) bytes, 256-byte aligned), and sum in fp32.  HPF_F32 (check mode): `weights`
  * is w itself, products and sums are in double.
- *   M <= 2^22, K, N <= 2^20 (else HPF_EUNSUPPORTED). */
+ *   M <= 2^21, K, N <= 2^20 (else HPF_EUNSUPPORTED). */
 typedef enum { HPF_ACT_NONE = 0, HPF_ACT_RELU = 1, HPF_ACT_GELU = 2 /* z * Phi(z) */, HPF_ACT_SILU = 3 /* z / (1 + exp(-z)) */ } hpf_activation;
 size_t hpf_op_linear_packed_bytes(int32_t K, int32_t N);
 hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed, size_t packed_bytes, void* hip_stream);
@@ -431,7 +431,8 @@ hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy,
                                   int32_t K, int32_t N, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Rows of logits.  dtype is the type of the logits and of gradients with respect to them; everything else is fp32 (or int32)
- * and statistics are held in fp32 or wider.  classes <= 2^28, lists of at most 64 entries (else HPF_EUNSUPPORTED).
+ * and statistics are held in fp32 or wider.  rows <= 2^21, classes <= 2^28, rows * classes <= 2^36, lists of at most 64 entries
+ * (else HPF_EUNSUPPORTED).
  * A logit of -infinity is a masked class: probability 0, never in a list.  A row of masked classes only takes no part: log
  * probabilities -infinity, entropy 0, loss 0, gradient 0.  A row with a NaN or +infinity gives NaN (rank and indices -1).
  * labels: int32 in [0, classes), or -1: the row has no label (log probability 0, rank -1, no term in a loss); any other

@@ -3,6 +3,10 @@
 // all classes but the one that holds the maximum, dot the sum of exp(s - m) (s - m).  With Z = 1 + rest, log Z = log1p(rest), so
 // that log p and 1 - p keep their digits where one class is all but certain, and the entropy log Z - dot / Z adds two terms that
 // are never negative.
+//
+// All of them are bound by reading the logits once (and writing the gradient once).  A row, or one part of it, is read into registers as
+// it is stored, 16 bytes per thread and unit, by one wave or by one work-group; every pass over it -- maximum, sums, list, gradient
+// -- then takes it from there.  Long rows of few are divided among work-groups whose records a second launch joins.
 #include "hpf_answer.h"
 #include "hpf_device.h"
 
@@ -10,23 +14,17 @@ namespace hpf {
 namespace {
 
 constexpr float INF = __builtin_huge_valf();
+constexpr float LOG2E = 1.44269504f;
+typedef unsigned long long Key;
+
+__device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7fc00000u); }
 
 struct RowSum {
   float m, rest, dot;
   static __device__ __forceinline__ RowSum none() { return RowSum{-INF, 0.f, 0.f}; }
-  __device__ __forceinline__ void add(float s) {
-    if (s == -INF) return;                     // a masked class
-    if (s > m) {
-      merge_into(RowSum{s, 0.f, 0.f});
-    } else {
-      const float e = expf(s - m);
-      rest += e;
-      dot += e > 0.f || e != e ? e * (s - m) : 0.f;
-    }
-  }
   // this, but seen from the larger maximum o.m
   __device__ __forceinline__ void merge_into(const RowSum& o) {
-    if (m == -INF) { const float r = rest; *this = o; rest += r; return; }   // r: 0, or NaN if a NaN came before the first number
+    if (m == -INF) { const float r = rest; *this = o; rest += r; return; }   // r: 0, or NaN if there was a NaN but no number
     const float d = m - o.m, e = expf(d), z = rest + 1.f;
     const float dd = e > 0.f || e != e ? e * (dot + d * z) : 0.f;
     rest = o.rest + z * e;
@@ -40,112 +38,414 @@ struct RowSum {
   }
   __device__ __forceinline__ bool broken() const { return rest != rest || dot != dot || m == INF; }   // NaN or +infinity in the row
   __device__ __forceinline__ bool empty() const { return m == -INF; }                                 // every class masked
-  __device__ __forceinline__ float log_rest() const { return log1pf(rest); }                          // log Z
 };
 
-template <class V>
-__device__ __forceinline__ V from_lane(const V& v, int lane) {
-  static_assert(sizeof(V) % 4 == 0, "whole registers");
-  V r;
-  const int* p = reinterpret_cast<const int*>(&v);
-  int* q = reinterpret_cast<int*>(&r);
-#pragma unroll
-  for (unsigned i = 0; i < sizeof(V) / 4; ++i) q[i] = __shfl(p[i], lane);
-  return r;
-}
-
-// over the 256 threads; every thread gets the result
-__device__ __forceinline__ RowSum block_sum(RowSum v, RowSum* sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int o = 32; o > 0; o >>= 1) {
-    const RowSum w = from_lane(v, lane ^ o);
-    if (lane & o) { RowSum t = w; t.merge(v); v = t; } else v.merge(w);   // one order for both
-  }
-  __syncthreads();
-  if (lane == 0) sh[wave] = v;
-  __syncthreads();
-  v = sh[0];
-  for (int i = 1; i < 4; ++i) v.merge(sh[i]);
-  return v;
-}
-
-// order of the list: larger value first, then lower index; 0 is behind every class
-__device__ __forceinline__ unsigned long long key_of(float s, int c) {
+// Order of the list: larger value first, then lower index.  An unmasked class has a number above 0 in the upper half; 0 stands for none.
+__device__ __forceinline__ unsigned order_of(float s) {
   const unsigned u = __float_as_uint(s + 0.f);   // -0 counts as 0
-  return (unsigned long long)(u ^ (u >> 31 ? 0xffffffffu : 0x80000000u)) << 32 | (0xffffffffu - (unsigned)c);
+  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
-__device__ __forceinline__ unsigned long long block_max(unsigned long long v, unsigned long long* sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int o = 32; o > 0; o >>= 1) {
-    const unsigned long long w = from_lane(v, lane ^ o);
-    v = w > v ? w : v;
+__device__ __forceinline__ Key key_of(float s, int c) { return (Key)order_of(s) << 32 | (0xffffffffu - (unsigned)c); }
+__device__ __forceinline__ int class_of(Key k) { return (int)(0xffffffffu - (unsigned)k); }
+__device__ __forceinline__ float value_of(Key k) {
+  const unsigned u = (unsigned)(k >> 32);
+  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
+__device__ __forceinline__ Key shfl_xor(Key v, int o) {
+  return (Key)(unsigned)__shfl_xor((int)(v >> 32), o) << 32 | (unsigned)__shfl_xor((int)(unsigned)v, o);
+}
+
+// NT threads that have a row together: 64 (a wave, with the LDS of its own that it is given) or a work-group.  LDS of a group:
+template <int NT>
+struct GroupSpace {
+  static constexpr int CANDIDATES = NT == 64 ? 512 : 2048;
+  float f[3][16];
+  int i[16], n;
+  unsigned i64[64], least;
+  Key waves[16], list[64], next[64], keys[CANDIDATES];
+};
+template <int NT>
+struct Group {
+  GroupSpace<NT>& sh;
+  int tid;      // 0 ... NT - 1
+  __device__ __forceinline__ void sync() const {
+    if (NT == 64) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); else __syncthreads();
   }
-  __syncthreads();
-  if (lane == 0) sh[wave] = v;
-  __syncthreads();
-  v = sh[0];
-  for (int i = 1; i < 4; ++i) v = sh[i] > v ? sh[i] : v;
-  return v;
+  // over all threads, the same order everywhere; every thread gets the results
+  template <int N, class OP>
+  __device__ __forceinline__ void reduce(float (&v)[N], OP op) const {
+    for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = op(v[k], __shfl_xor(v[k], o));
+    if (NT == 64) return;
+    __syncthreads();
+    if ((tid & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < N; ++k) sh.f[k][tid >> 6] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = sh.f[k][0];
+      for (int w = 1; w < NT / 64; ++w) v[k] = op(v[k], sh.f[k][w]);
+    }
+  }
+  __device__ __forceinline__ float max(float v) const {
+    float a[1] = {v};
+    reduce(a, [](float x, float y) { return fmaxf(x, y); });
+    return a[0];
+  }
+  // waves that counted the same number in all their lanes
+  __device__ __forceinline__ int total(int per_wave) const {
+    if (NT == 64) return per_wave;
+    __syncthreads();
+    if ((tid & 63) == 0) sh.i[tid >> 6] = per_wave;
+    __syncthreads();
+    int t = 0;
+    for (int w = 0; w < NT / 64; ++w) t += sh.i[w];
+    return t;
+  }
+  __device__ __forceinline__ Key max(Key v) const {
+    for (int o = 1; o < 64; o <<= 1) {
+      const Key w = shfl_xor(v, o);
+      v = w > v ? w : v;
+    }
+    if (NT == 64) return v;
+    __syncthreads();
+    if ((tid & 63) == 0) sh.waves[tid >> 6] = v;
+    __syncthreads();
+    v = sh.waves[0];
+    for (int w = 1; w < NT / 64; ++w) v = sh.waves[w] > v ? sh.waves[w] : v;
+    return v;
+  }
+  // The `top` largest of everybody's keys, in order, to out(j, key); 0 where there are no more.  mine: the order of this thread's largest
+  // value (0: none); each(f) calls f for all of its keys; at(i), i < n, are all keys once more (0: none), those of equal values in the order
+  // of their classes.  The top-th largest of 64 groups' maxima is a lower bound of the last entry: what is not below it is collected and
+  // ordered by counting.  Where that is too much, thousands of equal logits most likely, only what is above the bound is collected, and of
+  // those at the bound the first; where that is too much still, `top` rounds of maxima decide.
+  template <class EACH, class AT, class OUT>
+  __device__ __forceinline__ void select(int top, unsigned mine, EACH each, AT at, int n, OUT out) const {
+    constexpr int LANES = NT / 64;        // per group
+    unsigned g = mine;
+    for (int o = 1; o < LANES; o <<= 1) {
+      const unsigned w = (unsigned)__shfl_xor((int)g, o);
+      g = w > g ? w : g;
+    }
+    sync();
+    if (tid % LANES == 0) sh.i64[tid / LANES] = g;
+    sync();
+    if (tid < 64) {
+      g = sh.i64[tid];
+      int above = 0;                      // equal ones count in the order of the lanes
+      for (int i = 0; i < 64; ++i) {
+        const unsigned o = (unsigned)__builtin_amdgcn_readlane((int)g, i);
+        above += o > g || (o == g && i < tid);
+      }
+      if (above == top - 1) sh.least = g;
+    }
+    sync();
+    const unsigned least = sh.least < 1 ? 1 : sh.least;
+    auto collect = [&](Key k, unsigned border) {
+      if ((unsigned)(k >> 32) >= border) {
+        const int i = atomicAdd(&sh.n, 1);
+        if (i < GroupSpace<NT>::CANDIDATES) sh.keys[i] = k;
+      }
+    };
+    if (tid == 0) sh.n = 0;
+    sync();
+    if (mine >= least) each([&](Key k) { collect(k, least); });
+    sync();
+    int found = sh.n;
+    if (found > GroupSpace<NT>::CANDIDATES && least != 0xffffffffu) {
+      sync();
+      if (tid == 0) sh.n = 0;
+      sync();
+      for (int i = tid; i < n; i += NT) collect(at(i), least + 1);
+      sync();
+      found = sh.n;
+      const unsigned border = found <= GroupSpace<NT>::CANDIDATES - 64 ? least : 0;
+      for (int i0 = 0; border && i0 < n && found < top; i0 += NT) {      // the first ones at the bound
+        const Key k = i0 + tid < n ? at(i0 + tid) : 0;
+        const bool is = (unsigned)(k >> 32) == border;
+        const unsigned long long lanes = __ballot(is);
+        if (NT > 64) {
+          __syncthreads();
+          if ((tid & 63) == 0) sh.i[tid >> 6] = __popcll(lanes);
+          __syncthreads();
+        }
+        int place = found + __popcll(lanes & ((1ull << (tid & 63)) - 1)), all = 0;
+        if (NT > 64) {
+          for (int w = 0; w < NT / 64; ++w) {
+            if (w < tid >> 6) place += sh.i[w];
+            all += sh.i[w];
+          }
+        } else {
+          all = __popcll(lanes);
+        }
+        if (is && place < top) sh.keys[place] = k;
+        found = found + all < top ? found + all : top;
+      }
+      sync();
+    }
+    if (found <= GroupSpace<NT>::CANDIDATES) {
+      for (int i = tid; i < found; i += NT) {
+        const Key k = sh.keys[i];
+        int above = 0;
+        for (int j = 0; j < found; ++j) above += sh.keys[j] > k;
+        if (above < top) out(above, k);
+      }
+      for (int j = found + tid; j < top; j += NT) out(j, 0);
+    } else {
+      Key last = ~0ull;
+      for (int j = 0; j < top; ++j) {
+        Key best = 0;
+        for (int i = tid; i < n; i += NT) {
+          const Key k = at(i);
+          if (k < last && k > best) best = k;
+        }
+        last = max(best);
+        if (tid == 0) out(j, last);
+      }
+    }
+    sync();
+  }
+};
+
+// `len` elements from p on, held by NT threads as they are stored: unit j of thread t is 16-byte unit t + j * NT, counted from the 16-byte
+// boundary at or before p.  Elements before p or behind the end read as -infinity; units that lie across an end are read element by element.
+template <class T, int NT, int J>
+struct Held {
+  static constexpr int E = 16 / sizeof(T), CAPACITY = NT * J * E, UNITS = J, THREADS = NT;
+  uint32_t v[J][4];
+  int shift, len, tid;        // first element's place in its unit
+
+  __device__ __forceinline__ bool used(int j) const { return j * NT * E - shift < len; }      // uniform
+  __device__ __forceinline__ int first(int j) const { return (tid + j * NT) * E - shift; }
+  __device__ __forceinline__ bool inside(int j) const { const int e0 = first(j); return e0 >= 0 && e0 + E <= len; }
+
+  __device__ __forceinline__ void load(const T* p, int n, int t) {
+    shift = (int)(((uintptr_t)p & 15) / sizeof(T));
+    len = n;
+    tid = t;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (!used(j)) break;
+      const int e0 = first(j);
+      if (inside(j)) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p + e0);
+        v[j][0] = q.x; v[j][1] = q.y; v[j][2] = q.z; v[j][3] = q.w;
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[j][w] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+        if (e0 < len)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (e0 + e >= 0 && e0 + e < len) set(j, e, p[e0 + e]);
+      }
+    }
+  }
+  __device__ __forceinline__ void set(int j, int e, bf16_t x) { v[j][e >> 1] = e & 1 ? (v[j][e >> 1] & 0xffffu) | (uint32_t)x << 16 : (v[j][e >> 1] & 0xffff0000u) | x; }
+  __device__ __forceinline__ void set(int j, int e, float x) { v[j][e] = __float_as_uint(x); }
+  __device__ __forceinline__ float get(int j, int e) const {
+    if (sizeof(T) == 4) return __uint_as_float(v[j][e]);
+    return __uint_as_float(e & 1 ? v[j][e >> 1] & 0xffff0000u : v[j][e >> 1] << 16);
+  }
+  // A pass converts what is stored again: without this the compiler keeps the fp32 values of one pass for the next, twice the registers
+  __device__ __forceinline__ void renew(int j) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) asm("" : "+v"(v[j][w]));
+  }
+  // f(value, j, e) for all units in use
+  template <class F>
+  __device__ __forceinline__ void each(F f, bool fresh = true) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (!used(j)) break;
+      if (fresh) renew(j);
+#pragma unroll
+      for (int e = 0; e < E; ++e) f(get(j, e), j, e);
+    }
+  }
+  __device__ __forceinline__ float largest() {
+    float m = -INF;
+    each([&](float s, int, int) { m = fmaxf(m, s); });
+    return m;
+  }
+};
+
+// How many classes are before `label`, whose logit is `mine`: larger ones, and equal ones of lower index.  base: class of p's first element.
+// Counted per wave, one comparison per element: units before the label's take the next smaller number as their border.
+template <class H>
+__device__ __forceinline__ int count_before(H& h, int base, int label, float mine, int E) {
+  int n = 0;
+  const unsigned b = __float_as_uint(mine);
+  const bool exact = mine == -INF;             // a masked label, for which there is no smaller number
+  const float below = mine == 0.f ? -__uint_as_float(1) : __uint_as_float(mine > 0.f ? b - 1 : b + 1);
+  float border = 0.f;
+  h.each([&](float s, int j, int e) {
+    const int e0 = h.first(j);
+    if (e == 0) border = base + e0 + E <= label ? below : mine;
+    bool is = s > border;
+    if (exact) is = s > mine || (s == mine && e0 + e >= 0 && e0 + e < h.len && base + e0 + e < label);
+    n += __popcll(__ballot(is));
+  });
+  if (exact) return n;
+  // the label's own unit: equal logits in front of it, counted by the thread that holds it
+  const int at = label - base + h.shift;       // counted from the first unit's start
+  int more = 0;
+  if (at >= 0 && label - base < h.len)
+#pragma unroll
+    for (int j = 0; j < H::UNITS; ++j)
+      if (at / E == h.tid + j * H::THREADS)
+#pragma unroll
+        for (int e = 0; e < H::E; ++e) more += e < at % E && h.get(j, e) == mine;
+  for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o);
+  return n + more;
 }
 
-__device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7fc00000u); }
+// {m, rest, dot} of what a group holds.  Only waves that hold a maximum keep it apart from the sum.
+template <class T, int NT, int J>
+__device__ __forceinline__ RowSum sum_of(const Group<NT>& g, Held<T, NT, J>& h, float largest) {
+  const float m = g.max(largest), mm = m == -INF ? 0.f : m;
+  float v[3] = {0.f, 0.f, 0.f};                // rest, dot, classes at the maximum
+  if (NT == 64 || __any(largest == m)) {
+    h.each([&](float s, int, int) {
+      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * LOG2E);
+      v[0] += d == 0.f ? 0.f : e;
+      v[1] = fmaf(e, fmaxf(d, -3e38f), v[1]);
+      v[2] += d == 0.f ? 1.f : 0.f;
+    });
+  } else {
+    h.each([&](float s, int, int) {
+      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * LOG2E);
+      v[0] += e;
+      v[1] = fmaf(e, fmaxf(d, -3e38f), v[1]);
+    });
+  }
+  g.reduce(v, [](float a, float b) { return a + b; });
+  return RowSum{m, m == -INF ? v[0] : v[0] + (v[2] - 1.f), v[1]};
+}
 
+// ---- log probabilities ------------------------------------------------------------------------------------------------
+// What a part of a row leaves for the join: its sum, how many of its classes are before the label, its list
+struct PartRecord { RowSum sum; int before; };
+
+__device__ __forceinline__ void write_row(const LogprobForward& a, int row, const RowSum& v, int before, int label, bool has, float mine) {
+  const bool broken = v.broken();
+  const float lz = v.empty() ? -INF : log1pf(v.rest);
+  if (a.logprob)
+    a.logprob[row] = label == -1 ? 0.f : (broken || !has) ? quiet_nan() : v.empty() ? -INF : (float)((double)mine - v.m - log1p((double)v.rest));
+  if (a.rank) a.rank[row] = has && !broken ? before : -1;
+  if (a.entropy) a.entropy[row] = broken ? quiet_nan() : v.empty() ? 0.f : lz - v.dot / (1.f + v.rest);
+  if (a.stats) {
+    a.stats[2 * (long)row] = broken ? quiet_nan() : v.m;
+    a.stats[2 * (long)row + 1] = broken ? quiet_nan() : lz;
+  }
+}
+__device__ __forceinline__ void write_entry(const LogprobForward& a, int row, int j, Key k, const RowSum& v, float lz) {
+  const long at = (long)row * a.top + j;
+  const bool broken = v.broken();
+  a.top_index[at] = k && !broken ? class_of(k) : -1;
+  a.top_logprob[at] = broken ? quiet_nan() : k ? (value_of(k) - v.m) - lz : -INF;
+}
+
+// Group `part` of `parts` of a row takes every chunk of CAPACITY elements from part * per_part on
+template <class T, int NT, int J>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_logprob_forward(LogprobForward a, int parts, long per_part, PartRecord* records, Key* lists) {
+  typedef Held<T, NT, J> H;
+  constexpr int PER = NT < 256 ? 256 / NT : 1;         // rows per work-group
+  __shared__ GroupSpace<NT> space[PER];
+  const Group<NT> g{space[threadIdx.x / NT], (int)threadIdx.x % NT};
+  const long unit = (long)blockIdx.x * PER + threadIdx.x / NT;
+  const int row = (int)(unit / parts), part = (int)(unit - (long)row * parts);
+  if (row >= a.rows) return;                           // a whole wave, or nobody
+  const T* s = (const T*)a.logits + row * a.ld;
+  const int label = a.labels ? a.labels[row] : -1;
+  const bool has = label >= 0 && label < a.classes;
+  const float mine = has ? to_f32(s[label]) : INF;
+  const long c_begin = part * per_part, c_end = c_begin + per_part < a.classes ? c_begin + per_part : a.classes;
+  RowSum v = RowSum::none();
+  int before = 0;
+  Key held = 0;                                        // entry g.tid of the list of the chunks so far, which is in LDS too
+  int kept = 0;
+  long step;
+  H h;
+  for (long c0 = c_begin; c0 < c_end; c0 += step) {
+    const long room = H::CAPACITY - (long)(((uintptr_t)(s + c0) & 15) / sizeof(T));
+    step = c_end - c0 < room ? c_end - c0 : room;
+    h.load(s + c0, (int)step, g.tid);
+    const float largest = h.largest();
+    const RowSum w = sum_of(g, h, largest);
+    if (c0 == c_begin) v = w; else v.merge(w);
+    if (has) before += count_before(h, (int)c0, label, mine, H::E);
+    if (a.top) {
+      unsigned best = (unsigned)(held >> 32);
+      if (largest > -INF && order_of(largest) > best) best = order_of(largest);
+      const bool more = c0 + step < c_end;             // the list goes on, in LDS
+      const bool direct = parts == 1 && !more;
+      const float lz = v.empty() ? 0.f : log1pf(v.rest);
+#pragma unroll
+      for (int j = 0; j < J; ++j) h.renew(j);
+      g.select(a.top, best, [&](auto f) {
+        if (held) f(held);
+        h.each([&](float t, int j, int e) { if (t > -INF) f(key_of(t, (int)c0 + h.first(j) + e)); }, false);
+      }, [&](int i) -> Key {
+        if (i < a.top) return i < kept ? g.sh.list[i] : 0;           // classes of earlier chunks come first
+        const float t = to_f32(s[c0 + i - a.top]);
+        return t > -INF ? key_of(t, (int)c0 + i - a.top) : 0;
+      }, (int)step + a.top, [&](int j, Key k) {
+        if (direct) write_entry(a, row, j, k, v, lz);
+        else if (more) g.sh.next[j] = k;
+        else lists[unit * a.top + j] = k;
+      });
+      if (more) {
+        held = g.tid < a.top ? g.sh.next[g.tid] : 0;
+        if (g.tid < a.top) g.sh.list[g.tid] = held;
+        kept = a.top;
+        g.sync();
+      }
+    }
+  }
+  before = g.total(before);
+  if (g.tid) return;
+  if (parts == 1) write_row(a, row, v, before, label, has, mine);
+  else records[unit] = PartRecord{v, before};
+}
+
+// a.parts <= 256 records and lists of a row
 template <class T>
-__global__ __launch_bounds__(256) void k_logprob_forward(LogprobForward a) {
-  __shared__ RowSum sh[4];
-  __shared__ unsigned long long shk[4];
-  const int row = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int parts, const PartRecord* __restrict__ records, const Key* __restrict__ lists) {
+  __shared__ GroupSpace<256> space;
+  const Group<256> g{space, (int)threadIdx.x};
+  const int row = blockIdx.x;
   const T* s = (const T*)a.logits + row * a.ld;
   const int label = a.labels ? a.labels[row] : -1;
   const bool has = label >= 0 && label < a.classes;
   const float mine = has ? to_f32(s[label]) : 0.f;
+  __shared__ PartRecord rec[256];
+  if (g.tid < parts) rec[g.tid] = records[(long)row * parts + g.tid];
+  const Key* list = lists + (long)row * parts * a.top;
+  const int n = parts * a.top;
+  unsigned best = 0;
+  for (int i = g.tid; i < n; i += 256) best = (unsigned)(list[i] >> 32) > best ? (unsigned)(list[i] >> 32) : best;
+  __syncthreads();
   RowSum v = RowSum::none();
   int before = 0;
-  for (int c = tid; c < a.classes; c += 256) {
-    const float t = to_f32(s[c]);
-    v.add(t);
-    before += t > mine || (t == mine && c < label);
-  }
-  v = block_sum(v, sh);
-  const bool broken = v.broken();
-  __shared__ int total;
-  if (tid == 0) total = 0;
-  __syncthreads();
-  if (before) atomicAdd(&total, before);
-  __syncthreads();
-  if (tid == 0) {
-    const float lz = v.empty() ? -INF : v.log_rest();
-    if (a.logprob)
-      a.logprob[row] = label == -1 ? 0.f : (broken || !has) ? quiet_nan() : v.empty() ? -INF : (float)((double)mine - v.m - log1p((double)v.rest));
-    if (a.rank) a.rank[row] = has && !broken ? total : -1;
-    if (a.entropy) a.entropy[row] = broken ? quiet_nan() : v.empty() ? 0.f : lz - v.dot / (1.f + v.rest);
-    if (a.stats) {
-      a.stats[2 * (long)row] = broken ? quiet_nan() : v.m;
-      a.stats[2 * (long)row + 1] = broken ? quiet_nan() : lz;
-    }
-  }
-  unsigned long long last = ~0ull;
-  for (int j = 0; j < a.top; ++j) {
-    unsigned long long best = 0;
-    if (!broken && last)
-      for (int c = tid; c < a.classes; c += 256) {
-        const float t = to_f32(s[c]);
-        const unsigned long long k = t == -INF ? 0 : key_of(t, c);
-        if (k < last && k > best) best = k;
-      }
-    last = block_max(best, shk);
-    if (tid == 0) {
-      const int c = (int)(0xffffffffu - (unsigned)last);
-      const long at = (long)row * a.top + j;
-      a.top_index[at] = last ? c : -1;
-      a.top_logprob[at] = broken ? quiet_nan() : last ? (float)((double)to_f32(s[c]) - v.m - log1p((double)v.rest)) : -INF;
-    }
-  }
+  for (int i = 0; i < parts; ++i) { v.merge(rec[i].sum); before += rec[i].before; }
+  if (g.tid == 0) write_row(a, row, v, before, label, has, mine);
+  if (!a.top) return;
+  const float lz = v.empty() ? 0.f : log1pf(v.rest);
+  g.select(a.top, best, [&](auto f) { for (int i = g.tid; i < n; i += 256) if (list[i]) f(list[i]); },
+           [&](int i) { return list[i]; }, n, [&](int j, Key k) { write_entry(a, row, j, k, v, lz); });
 }
 
+// ---- gradient of log probability and entropy ---------------------------------------------------------------------------
+// 16-byte units of all rows, one after the other; where logits and dlogits do not share their place within a unit, element by element
 template <class T>
-__global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a) {
-  const int row = blockIdx.x;
+__global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a, unsigned blocks_per_row) {
+  constexpr int E = 16 / sizeof(T), U = 4;
+  const int row = (int)(blockIdx.x / blocks_per_row);
+  const int b = (int)(blockIdx.x - (unsigned)row * blocks_per_row);
   const T* s = (const T*)a.logits + row * a.ld;
   T* d = (T*)a.dlogits + row * a.ldd;
   const int label = a.labels ? a.labels[row] : -1;
@@ -153,22 +453,59 @@ __global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a) {
   float g = a.grad_logprob && label != -1 ? a.grad_logprob[row] : 0.f;
   if (label < -1 || label >= a.classes) g = quiet_nan();
   const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.f, h = a.grad_entropy ? a.entropy[row] : 0.f;
-  for (int c = threadIdx.x; c < a.classes; c += 256) {
-    const float logp = (to_f32(s[c]) - m) - lz;
-    const float p = expf(logp);
-    float v = c == label ? -g * expm1f(logp) : -g * p;
-    if (p > 0.f || p != p) v -= gh * p * (logp + h);
-    from_f32(d + c, m == -INF ? 0.f : v);
+  auto grad = [&](float x, int c) {
+    const float logp = (x - m) - lz, p = __builtin_amdgcn_exp2f(logp * LOG2E);
+    // p = 0: the class is masked or as good as that; its entropy term is p log p -> 0
+    float v = fmaf(-gh * p, fmaxf(logp, -3e38f) + h, -g * p);
+    if (c == label) v = fmaf(-gh * p, fmaxf(logp, -3e38f) + h, -g * expm1f(logp));
+    return m == -INF ? 0.f : v;
+  };
+  const int shift = (int)(((uintptr_t)s & 15) / sizeof(T));
+  const bool alike = (((uintptr_t)s ^ (uintptr_t)d) & 15) == 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long e0 = ((long)b * (256 * U) + u * 256 + threadIdx.x) * E - shift;
+    if (e0 >= a.classes) break;
+    if (alike && e0 >= 0 && e0 + E <= a.classes) {
+      float x[8];
+      if (sizeof(T) == 2) {
+        load8((const bf16_t*)s + e0, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = grad(x[e], (int)e0 + e);
+        store8((bf16_t*)d + e0, x);
+      } else {
+        float4 q = *reinterpret_cast<const float4*>((const float*)s + e0);
+        q = make_float4(grad(q.x, (int)e0), grad(q.y, (int)e0 + 1), grad(q.z, (int)e0 + 2), grad(q.w, (int)e0 + 3));
+        *reinterpret_cast<float4*>((float*)d + e0) = q;
+      }
+    } else {
+      for (int e = 0; e < E; ++e)
+        if (e0 + e >= 0 && e0 + e < a.classes) from_f32(d + e0 + e, grad(to_f32(s[e0 + e]), (int)e0 + e));
+    }
   }
 }
 
+// ---- distillation --------------------------------------------------------------------------------------------------
 // sums over the wave, in double; every lane gets the result
 __device__ __forceinline__ double wave_sum(double v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
 
-// What a row's list says, one entry per lane: the loss's soft part and the gradient at the listed classes
+// What the student's row leaves for the loss: the maximum and the sums of the other classes at temperature 1 and T
+struct Soft { float m, rest1, restt; };
+__device__ __forceinline__ void merge(Soft& v, const Soft& o, float it) {
+  RowSum a{v.m, v.rest1, 0.f};
+  a.merge(RowSum{o.m, o.rest1, 0.f});
+  // at temperature T the distance of the maxima counts 1 / T of itself
+  float t;
+  if (v.m == -INF || o.m == -INF) t = v.restt + o.restt;     // of a part of masked classes: 0, or NaN
+  else if (v.m >= o.m) t = v.restt + (1.f + o.restt) * expf((o.m - v.m) * it);
+  else t = o.restt + (1.f + v.restt) * expf((v.m - o.m) * it);
+  v = Soft{a.m, a.rest, t};
+}
+
+// What a row's list says, one entry per lane, by one wave: the loss's soft part and the gradient at the listed classes
 struct List {
   bool on, some, broken;     // entry there; any entry there; an index outside the classes
   int index;
@@ -176,7 +513,7 @@ struct List {
   double diff;               // q_c - P_c, P_c: probability of the entry's class in the list (all entries of that class)
 };
 template <class T>
-__device__ __forceinline__ List read_list(const Distill& a, const T* s, int row, const RowSum& v, int lane) {
+__device__ __forceinline__ List read_list(const Distill& a, const T* s, int row, const Soft& v, int lane) {
   List l{};
   const long at = (long)row * a.top + lane;
   l.index = lane < a.top ? a.top_index[at] : -1;
@@ -192,7 +529,7 @@ __device__ __forceinline__ List read_list(const Distill& a, const T* s, int row,
   const double z = wave_sum(e);
   const double p = e / z;
   const double logp = (t - top) * it - log(z);
-  const double logq = in ? ((double)to_f32(s[l.index]) - v.m) * it - log1p((double)v.rest) : 0.0;
+  const double logq = in ? ((double)to_f32(s[l.index]) - v.m) * it - log1p((double)v.restt) : 0.0;
   l.soft = wave_sum(l.on && p != 0.0 ? p * (logp - logq) : 0.0);
   double same = 0.0;
   for (int j = 0; j < a.top; ++j) {
@@ -203,91 +540,294 @@ __device__ __forceinline__ List read_list(const Distill& a, const T* s, int row,
   return l;
 }
 
+// Sums of what a group holds at temperatures 1 (if HARD) and T
+template <bool HARD, class T, int NT, int J>
+__device__ __forceinline__ Soft soft_of(const Group<NT>& g, Held<T, NT, J>& h, float it) {
+  const float largest = h.largest(), m = g.max(largest), mm = m == -INF ? 0.f : m, ct = LOG2E * it;
+  float v[3] = {0.f, 0.f, 0.f};                // rest at T, rest at 1, classes at the maximum
+  if (NT == 64 || __any(largest == m)) {
+    h.each([&](float s, int, int) {
+      const float d = s - mm;
+      v[0] += d == 0.f ? 0.f : __builtin_amdgcn_exp2f(d * ct);
+      if (HARD) v[1] += d == 0.f ? 0.f : __builtin_amdgcn_exp2f(d * LOG2E);
+      v[2] += d == 0.f ? 1.f : 0.f;
+    });
+  } else {
+    h.each([&](float s, int, int) {
+      const float d = s - mm;
+      v[0] += __builtin_amdgcn_exp2f(d * ct);
+      if (HARD) v[1] += __builtin_amdgcn_exp2f(d * LOG2E);
+    });
+  }
+  g.reduce(v, [](float a, float b) { return a + b; });
+  const float ties = m == -INF ? 0.f : v[2] - 1.f;
+  return Soft{m, v[1] + ties, v[0] + ties};
+}
+
+// Loss of a row, its gradient's factors, and the entries that are taken from the logarithms
 template <class T>
-__global__ __launch_bounds__(256) void k_distill(Distill a) {
-  __shared__ RowSum sh[4];
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const T* s = (const T*)a.logits + row * a.ld;
-  const float it = 1.f / a.temperature;
-  RowSum v1 = RowSum::none(), vt = RowSum::none();   // at temperature 1 and T; the maxima are those of the logits
-  for (int c = tid; c < a.classes; c += 256) {
-    const float t = to_f32(s[c]);
-    v1.add(t);
+struct Answer {
+  const Distill& a;
+  const T* s;
+  int row, label;
+  bool has, bad, empty;
+  double logl, ws, wh;       // log softmax at the label; weights of the soft and the hard term
+  float fs, fh;              // the same over Z
+  Soft v;
+
+  __device__ __forceinline__ Answer(const Distill& a_, const T* s_, int row_, const Soft& v_, bool some, bool list_broken) : a(a_), s(s_), row(row_), v(v_) {
+    label = a.labels ? a.labels[row] : -1;
+    has = label >= 0 && label < a.classes;
+    const bool hard = a.hard_weight != 0.f;
+    empty = v.m == -INF;
+    bad = v.m == INF || v.restt != v.restt || (hard && v.rest1 != v.rest1) || list_broken || (label != -1 && !has);
+    const double hw = (double)a.hard_weight, w = a.row_weight ? (double)a.row_weight[row] : 1.0;
+    logl = has && hard ? (double)to_f32(s[label]) - v.m - log1p((double)v.rest1) : 0.0;
+    ws = some ? w * (1.0 - hw) * a.temperature : 0.0;
+    wh = has ? w * hw : 0.0;
+    fs = bad ? quiet_nan() : (float)(ws / (1.0 + v.restt));
+    fh = bad ? quiet_nan() : hard ? (float)(wh / (1.0 + v.rest1)) : 0.f;
   }
-  v1 = block_sum(v1, sh);
-  const bool broken = v1.broken(), empty = v1.empty();
-  float z = 0.f;
-  int ties = 0;
-  for (int c = tid; c < a.classes; c += 256) {
-    const float t = to_f32(s[c]);
-    if (t == v1.m) ++ties;
-    else z += expf((t - v1.m) * it);
-  }
-  __shared__ float zs[256];
-  __shared__ int ts[256];
-  zs[tid] = z; ts[tid] = ties;
-  __syncthreads();
-  for (int o = 128; o > 0; o >>= 1) {
-    if (tid < o) { zs[tid] += zs[tid + o]; ts[tid] += ts[tid + o]; }
-    __syncthreads();
-  }
-  vt.m = v1.m;
-  vt.rest = zs[0] + (float)(ts[0] - 1);
-  const int label = a.labels ? a.labels[row] : -1;
-  const bool has = label >= 0 && label < a.classes;
-  const List l = read_list(a, s, row, vt, lane);
-  const bool bad = broken || l.broken || (label != -1 && !has);
-  const double logl = has ? (double)to_f32(s[label]) - v1.m - log1p((double)v1.rest) : 0.0;
-  const double hw = (double)a.hard_weight, T2 = (double)a.temperature * a.temperature;
-  if (tid == 0) {
+  __device__ __forceinline__ void write_loss(const List& l) const {
+    const double hw = (double)a.hard_weight;
     double loss = 0.0;
-    if (l.some && hw != 1.0) loss += (1.0 - hw) * T2 * l.soft;
+    if (l.some && hw != 1.0) loss += (1.0 - hw) * a.temperature * a.temperature * l.soft;
     if (has && hw != 0.0) loss -= hw * logl;
     a.loss[row] = bad ? quiet_nan() : empty ? 0.f : (float)loss;
   }
+  // the gradient at the listed classes and the label, where q - p and p - 1 may cancel, among classes [c0, c1); by one wave
+  __device__ __forceinline__ void write_entries(const List& l, T* d, long c0, long c1, int lane) const {
+    if (bad || empty) return;
+    const double it = 1.0 / (double)a.temperature;
+    const bool listed = __any(l.on && l.index == label);
+    if (l.on && l.index >= c0 && l.index < c1) {
+      const double t = (double)to_f32(s[l.index]) - v.m;
+      const double hard = wh == 0.0 ? 0.0 : l.index == label ? expm1(logl) : exp(t - log1p((double)v.rest1));
+      from_f32(d + l.index, (float)(ws * l.diff + wh * hard));
+    }
+    if (has && !listed && label >= c0 && label < c1 && lane == 0) {
+      const double q = exp(((double)to_f32(s[label]) - v.m) * it - log1p((double)v.restt));
+      from_f32(d + label, (float)(ws * q + wh * expm1(logl)));
+    }
+  }
+};
+
+// gradient of the `len` held elements to d
+template <bool HARD, class T, int NT, int J>
+__device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero) {
+  typedef Held<T, NT, J> H;
+  const float ct = LOG2E * it;
+  const bool alike = (int)(((uintptr_t)d & 15) / sizeof(T)) == h.shift;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    if (!h.used(j)) break;
+    h.renew(j);
+    float x[H::E];
+#pragma unroll
+    for (int e = 0; e < H::E; ++e) {
+      const float t = h.get(j, e) - m;
+      x[e] = fs * __builtin_amdgcn_exp2f(t * ct);
+      if (HARD) x[e] = fmaf(fh, __builtin_amdgcn_exp2f(t * LOG2E), x[e]);
+      if (zero) x[e] = 0.f;
+    }
+    const int e0 = h.first(j);
+    if (alike && h.inside(j)) {
+      if (sizeof(T) == 2) {
+        uint4 q;
+        q.x = pack_bf16x2(x[0], x[1]); q.y = pack_bf16x2(x[2], x[3]);
+        q.z = pack_bf16x2(x[H::E - 4], x[H::E - 3]); q.w = pack_bf16x2(x[H::E - 2], x[H::E - 1]);
+        *reinterpret_cast<uint4*>(d + e0) = q;
+      } else {
+        *reinterpret_cast<float4*>(d + e0) = make_float4(x[0], x[1], x[2], x[3]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < H::E; ++e)
+        if (e0 + e >= 0 && e0 + e < h.len) from_f32(d + e0 + e, x[e]);
+    }
+  }
+}
+
+// a row that a group holds whole
+template <bool HARD, class T, int NT, int J>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill(Distill a) {
+  constexpr int PER = NT < 256 ? 256 / NT : 1;
+  __shared__ GroupSpace<NT> space[PER];
+  const Group<NT> g{space[threadIdx.x / NT], (int)threadIdx.x % NT};
+  const int row = blockIdx.x * PER + threadIdx.x / NT;
+  if (row >= a.rows) return;
+  const T* s = (const T*)a.logits + row * a.ld;
+  const float it = 1.f / a.temperature;
+  Held<T, NT, J> h;
+  h.load(s, a.classes, g.tid);
+  const Soft v = soft_of<HARD>(g, h, it);
+  // every wave needs to know whether the list has entries and bad ones; the first one reads it
+  List l{};
+  if (g.tid < 64) {
+    l = read_list(a, s, row, v, g.tid);
+    if (NT > 64 && g.tid == 0) g.sh.n = (int)l.some | (int)l.broken << 1;
+  }
+  bool some = l.some, broken = l.broken;
+  if (NT > 64) {
+    __syncthreads();
+    some = g.sh.n & 1;
+    broken = g.sh.n & 2;
+  }
+  const Answer<T> ans(a, s, row, v, some, broken);
+  if (g.tid == 0) ans.write_loss(l);
   if (!a.dlogits) return;
   T* d = (T*)a.dlogits + row * a.ldd;
-  const double w = a.row_weight ? (double)a.row_weight[row] : 1.0;
-  const double ws = l.some ? w * (1.0 - hw) * a.temperature : 0.0, wh = has ? w * hw : 0.0;
-  const float fs = bad ? quiet_nan() : (float)(ws / (1.0 + vt.rest)), fh = bad ? quiet_nan() : (float)(wh / (1.0 + v1.rest));
-  for (int c = tid; c < a.classes; c += 256) {
-    const float t = to_f32(s[c]) - v1.m;
-    from_f32(d + c, empty && !bad ? 0.f : fs * expf(t * it) + fh * expf(t));
+  write_gradient<HARD>(h, d, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad);
+  if (NT > 64) __syncthreads(); else __builtin_amdgcn_s_waitcnt(0x0f70);   // the stores above are done before the entries replace some of them
+  if (g.tid < 64) ans.write_entries(l, d, 0, a.classes, g.tid);
+}
+
+// a row divided among work-groups: first their sums ...
+template <bool HARD, class T, int J>
+__global__ __launch_bounds__(256) void k_distill_part(Distill a, int parts, long per_part, Soft* records) {
+  typedef Held<T, 256, J> H;
+  __shared__ GroupSpace<256> space;
+  const Group<256> g{space, (int)threadIdx.x};
+  const int row = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - (unsigned)row * parts);
+  const T* s = (const T*)a.logits + row * a.ld;
+  const float it = 1.f / a.temperature;
+  const long c_begin = part * per_part, c_end = c_begin + per_part < a.classes ? c_begin + per_part : a.classes;
+  Soft v{-INF, 0.f, 0.f};
+  long step;
+  for (long c0 = c_begin; c0 < c_end; c0 += step) {
+    const long room = H::CAPACITY - (long)(((uintptr_t)(s + c0) & 15) / sizeof(T));
+    step = c_end - c0 < room ? c_end - c0 : room;
+    H h;
+    h.load(s + c0, (int)step, g.tid);
+    const Soft w = soft_of<HARD>(g, h, it);
+    if (c0 == c_begin) v = w; else merge(v, w, it);
   }
-  if (bad || empty) return;
-  __syncthreads();             // the stores above are done before the entries below replace some of them
-  if (tid >= 64) return;
-  // at the listed classes and the label q - p and p - 1 are taken from the logarithms
-  const bool listed = __any(l.on && l.index == label);
-  if (l.on) {
-    const double t = (double)to_f32(s[l.index]) - v1.m;
-    const double hard = l.index == label ? expm1(logl) : exp(t - log1p((double)v1.rest));
-    from_f32(d + l.index, (float)(ws * l.diff + wh * hard));
+  if (g.tid == 0) records[blockIdx.x] = v;
+}
+// ... then loss and gradient
+template <bool HARD, class T, int J>
+__global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long per_part, const Soft* __restrict__ records) {
+  typedef Held<T, 256, J> H;
+  __shared__ Soft rec[256];
+  const int row = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - (unsigned)row * parts), tid = threadIdx.x;
+  const T* s = (const T*)a.logits + row * a.ld;
+  const float it = 1.f / a.temperature;
+  if (tid < parts) rec[tid] = records[(long)row * parts + tid];
+  __syncthreads();
+  Soft v = rec[0];
+  for (int i = 1; i < parts; ++i) merge(v, rec[i], it);
+  const List l = read_list(a, s, row, v, tid & 63);
+  const Answer<T> ans(a, s, row, v, l.some, l.broken);
+  if (part == 0 && tid == 0) ans.write_loss(l);
+  if (!a.dlogits) return;
+  T* d = (T*)a.dlogits + row * a.ldd;
+  const long c_begin = part * per_part, c_end = c_begin + per_part < a.classes ? c_begin + per_part : a.classes;
+  long step;
+  for (long c0 = c_begin; c0 < c_end; c0 += step) {
+    const long room = H::CAPACITY - (long)(((uintptr_t)(s + c0) & 15) / sizeof(T));
+    step = c_end - c0 < room ? c_end - c0 : room;
+    H h;
+    h.load(s + c0, (int)step, tid);
+    write_gradient<HARD>(h, d + c0, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad);
   }
-  if (has && !listed && lane == 0) {
-    const double q = exp(((double)to_f32(s[label]) - v1.m) * it - log1p((double)vt.rest));
-    from_f32(d + label, (float)(ws * q + wh * expm1(logl)));
+  __syncthreads();
+  if (tid < 64) ans.write_entries(l, d, c_begin, c_end, tid);
+}
+
+// ---- how rows are cut ------------------------------------------------------------------------------------------------
+constexpr int CUS = 256, MAX_PARTS = 256, PART_J = 4;
+
+struct RowCut {
+  int parts;
+  long per_part;                 // classes
+  int units;                     // 16-byte units of a row, with the one that a row across a boundary has more
+};
+// A row of 2048 units (32 KiB) and more is divided if there are not enough rows for all CUs, and if no work-group holds it (a part of it may
+// then need several chunks).
+// aligned: every row starts on 16 bytes (a workspace is sized for rows that do not, which never have fewer parts).
+RowCut row_cut(int dt, int rows, int classes, bool aligned) {
+  const int E = dt == DT_BF16 ? 8 : 4;
+  RowCut c;
+  c.units = (classes + E - 1) / E + (aligned ? 0 : 1);
+  const bool too_long = c.units > 1024 * 16;
+  c.parts = 1;
+  if (too_long || (rows <= CUS / 2 && c.units >= 2048)) {
+    long p = (2 * CUS + rows - 1) / rows;
+    const long most = c.units / 512;
+    if (p > most) p = most;
+    if (p > MAX_PARTS) p = MAX_PARTS;
+    if (p < 2) p = 2;
+    c.parts = (int)p;
   }
+  c.per_part = ((classes + c.parts - 1) / c.parts + 63) / 64 * 64;
+  c.parts = (int)((classes + c.per_part - 1) / c.per_part);     // none without classes
+  return c;
+}
+
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+bool aligned16(const void* p, long ld, size_t elem) { return ((uintptr_t)p & 15) == 0 && ((size_t)ld * elem & 15) == 0; }
+
+template <class T>
+hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hipStream_t s) {
+  const RowCut c = row_cut(dt, a.rows, a.classes, aligned16(a.logits, a.ld, sizeof(T)));
+  if (c.parts > 1) {
+    const unsigned n = (unsigned)((long)a.rows * c.parts);
+    PartRecord* records = (PartRecord*)workspace;
+    Key* lists = (Key*)((char*)workspace + align256((size_t)n * sizeof(PartRecord)));
+    k_logprob_forward<T, 256, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records, lists);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    k_logprob_join<T><<<(unsigned)a.rows, 256, 0, s>>>(a, c.parts, records, lists);
+  } else if (c.units <= 64 * 4) k_logprob_forward<T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
+  else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
+  else if (c.units <= 1024 * 8) k_logprob_forward<T, 1024, 8><<<(unsigned)a.rows, 1024, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
+  else k_logprob_forward<T, 1024, 16><<<(unsigned)a.rows, 1024, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t logprob_backward(const LogprobBackward& a, hipStream_t s) {
+  const long units = (a.classes + 16 / (long)sizeof(T) - 1) / (16 / (long)sizeof(T)) + 1;
+  const unsigned per_row = (unsigned)((units + 1023) / 1024);
+  k_logprob_backward<T><<<(unsigned)a.rows * per_row, 256, 0, s>>>(a, per_row);
+  return hipGetLastError();
+}
+
+template <bool HARD, class T>
+hipError_t distill(int dt, const Distill& a, void* workspace, hipStream_t s) {
+  const RowCut c = row_cut(dt, a.rows, a.classes, aligned16(a.logits, a.ld, sizeof(T)));
+  if (c.parts > 1) {
+    const unsigned n = (unsigned)((long)a.rows * c.parts);
+    Soft* records = (Soft*)workspace;
+    k_distill_part<HARD, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    k_distill_join<HARD, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
+  } else if (c.units <= 64 * 4) k_distill<HARD, T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
+  else if (c.units <= 256 * 8) k_distill<HARD, T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
+  else if (c.units <= 1024 * 8) k_distill<HARD, T, 1024, 8><<<(unsigned)a.rows, 1024, 0, s>>>(a);
+  else k_distill<HARD, T, 1024, 16><<<(unsigned)a.rows, 1024, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t logits_workspace_bytes(int, int, int, int) { return 0; }
+size_t logits_workspace_bytes(int dt, int rows, int classes, int top) {
+  const RowCut c = row_cut(dt, rows, classes, false);
+  const size_t n = (size_t)rows * c.parts;
+  return c.parts > 1 ? align256(n * sizeof(PartRecord)) + align256(n * top * sizeof(Key)) : 0;
+}
 
-hipError_t launch_logprob_forward(int dt, const LogprobForward& a, void*, hipStream_t stream) {
-  if (dt == DT_BF16) k_logprob_forward<bf16_t><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  else k_logprob_forward<float><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  return hipGetLastError();
+hipError_t launch_logprob_forward(int dt, const LogprobForward& a, void* workspace, hipStream_t stream) {
+  return dt == DT_BF16 ? logprob_forward<bf16_t>(dt, a, workspace, stream) : logprob_forward<float>(dt, a, workspace, stream);
 }
 hipError_t launch_logprob_backward(int dt, const LogprobBackward& a, hipStream_t stream) {
-  if (dt == DT_BF16) k_logprob_backward<bf16_t><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  else k_logprob_backward<float><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  return hipGetLastError();
+  return dt == DT_BF16 ? logprob_backward<bf16_t>(a, stream) : logprob_backward<float>(a, stream);
 }
-hipError_t launch_distill(int dt, const Distill& a, void*, hipStream_t stream) {
-  if (dt == DT_BF16) k_distill<bf16_t><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  else k_distill<float><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  return hipGetLastError();
+hipError_t launch_distill(int dt, const Distill& a, void* workspace, hipStream_t stream) {
+  const bool hard = a.hard_weight != 0.f;
+  if (dt == DT_BF16) return hard ? distill<true, bf16_t>(dt, a, workspace, stream) : distill<false, bf16_t>(dt, a, workspace, stream);
+  return hard ? distill<true, float>(dt, a, workspace, stream) : distill<false, float>(dt, a, workspace, stream);
 }
 
 }  // namespace hpf

@@ -27,7 +27,7 @@ hpf_status launched(hipError_t e) { return e == hipSuccess ? HPF_OK : fail(HPF_E
 hpf_status linear_shape(hpf_dtype dtype, int32_t M, int32_t K, int32_t N, int& dt) {
   if (!type_of(dtype, dt)) return fail(HPF_EINVAL, "unknown dtype");
   if (M < 0 || K < 1 || N < 1) return fail(HPF_EINVAL, "M must not be negative, K and N must be positive (%d, %d, %d)", M, K, N);
-  if (K > MAX_WIDTH || N > MAX_WIDTH || M > (1 << 22)) return fail(HPF_EUNSUPPORTED, "more than 2^22 rows or 2^20 columns (%d, %d, %d)", M, K, N);
+  if (K > MAX_WIDTH || N > MAX_WIDTH || M > (1 << 21)) return fail(HPF_EUNSUPPORTED, "more than 2^21 rows or 2^20 columns (%d, %d, %d)", M, K, N);
   return HPF_OK;
 }
 hpf_status workspace_ok(const void* workspace, size_t bytes, size_t need) {
@@ -125,7 +125,8 @@ hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy,
 static hpf_status logits_shape(hpf_dtype dtype, const void* logits, int64_t ld, int32_t top, int32_t rows, int32_t classes, int& dt) {
   if (!type_of(dtype, dt)) return fail(HPF_EINVAL, "unknown dtype");
   if (rows < 0 || classes < 1) return fail(HPF_EINVAL, "rows must not be negative, classes must be positive (%d, %d)", rows, classes);
-  if (classes > MAX_CLASSES) return fail(HPF_EUNSUPPORTED, "more than 2^28 classes");
+  if (rows > (1 << 21) || classes > MAX_CLASSES || (int64_t)rows * classes > (int64_t)1 << 36)
+    return fail(HPF_EUNSUPPORTED, "more than 2^21 rows, 2^28 classes or 2^36 logits (%d, %d)", rows, classes);
   if (top < 0) return fail(HPF_EINVAL, "negative list length");
   if (top > TOP_MAX) return fail(HPF_EUNSUPPORTED, "a list of %d entries, at most %d", top, TOP_MAX);
   if (rows == 0) return HPF_OK;
@@ -137,7 +138,7 @@ static hpf_status logits_shape(hpf_dtype dtype, const void* logits, int64_t ld, 
 
 size_t hpf_op_logits_workspace_bytes(hpf_dtype dtype, int32_t rows, int32_t classes, int32_t top) {
   int dt;
-  if (!type_of(dtype, dt) || rows < 1 || classes < 1 || classes > MAX_CLASSES || top < 0 || top > TOP_MAX) return 0;
+  if (!type_of(dtype, dt) || rows < 1 || rows > (1 << 21) || classes < 1 || classes > MAX_CLASSES || top < 0 || top > TOP_MAX) return 0;
   return logits_workspace_bytes(dt, rows, classes, top);
 }
 

@@ -50,7 +50,7 @@ def test_linear_refusals(hpf):
         g(EINVAL, "positive", K=0)
         g(EINVAL, "positive", N=0)
         g(EUN, "2^20", K=(1 << 20) + 1)
-        g(EUN, "2^22", M=(1 << 22) + 1)
+        g(EUN, "2^21", M=(1 << 21) + 1)
         g(EINVAL, "stride", ldx=15)
         g(EINVAL, "aligned", x=A + 1 if g is f else B + 1)
         g(EINVAL, "256-byte", w=(B if g is f else D) + 64)
@@ -117,6 +117,8 @@ def test_logits_refusals(hpf):
         g(EINVAL, "negative", rows=-1)
         g(EINVAL, "positive", classes=0)
         g(EUN, "2^28", classes=(1 << 28) + 1, ld=1 << 30)
+        g(EUN, "2^21", rows=(1 << 21) + 1)
+        g(EUN, "2^36", rows=1 << 20, classes=1 << 17, ld=1 << 17)
         g(EINVAL, "null", s=0)
         g(EINVAL, "stride", ld=9)
         g(EINVAL, "aligned", s=A + 1)

@@ -431,3 +431,25 @@ def test_streams_and_graphs(env, shape):
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, want[i]))
         assert all(torch.equal(p, q) for p, q in zip(every(*data[i]), want[i]))
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("classes,period,part,top", [(1020, 256, 80, 30), (2040, 512, 160, 30), (7900, 1024, 192, 20), (16000, 2048, 384, 20), (65000, 4096, 128, 5),
+                                                     (131072, 8192, 256, 5), (200001, 1024, 192, 40)])
+def test_lists_among_thousands_of_large_logits(env, mode, classes, period, part, top):
+    """Large logits in the first `part` classes of every `period` and small ones elsewhere: whole threads hold nothing else, and no simple
+    bound separates the list from the rest.  Distinct values, then many equal ones."""
+    hpf, torch, ops = env
+    g = torch.Generator(device="cuda").manual_seed(classes)
+    c = torch.arange(classes, device="cuda")
+    s = torch.randn(4, classes, device="cuda", generator=g)
+    large = (c % period) < part
+    s[:2] += 30.0 * large
+    s[1:3] = s[1:3].round()
+    s[3] = torch.where(large, 7.0, 6.0)
+    s = s.to(torch.bfloat16 if mode == "bf16" else torch.float32)
+    labels = torch.tensor([0, classes - 1, 5, classes // 2], device="cuda", dtype=torch.int32)
+    for n in (top, 64):
+        check_forward(torch, s, labels, n, ops[mode].logprob_forward(s, labels, n))
+    views = torch.cat([torch.zeros(4, 3, device="cuda", dtype=s.dtype), s], 1)[:, 3:]
+    check_forward(torch, views, labels, top, ops[mode].logprob_forward(views, labels, top))
