@@ -7,6 +7,8 @@
 // All of them are bound by reading the logits once (and writing the gradient once).  A row, or one part of it, is read into registers as
 // it is stored, 16 bytes per thread and unit, by one wave or by one work-group; every pass over it -- maximum, sums, list, gradient
 // -- then takes it from there.  Long rows of few are divided among work-groups whose records a second launch joins.
+#include <type_traits>
+
 #include "hpf_answer.h"
 #include "hpf_device.h"
 
@@ -45,16 +47,59 @@ __device__ __forceinline__ unsigned order_of(float s) {
   const unsigned u = __float_as_uint(s + 0.f);   // -0 counts as 0
   return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
+constexpr unsigned LOWEST = 0x00800000u;           // order of the lowest finite number
+__device__ __forceinline__ float value_at(unsigned order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 __device__ __forceinline__ Key key_of(float s, int c) { return (Key)order_of(s) << 32 | (0xffffffffu - (unsigned)c); }
 __device__ __forceinline__ int class_of(Key k) { return (int)(0xffffffffu - (unsigned)k); }
-__device__ __forceinline__ float value_of(Key k) {
-  const unsigned u = (unsigned)(k >> 32);
-  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
-}
+__device__ __forceinline__ float value_of(Key k) { return value_at((unsigned)(k >> 32)); }
 
 __device__ __forceinline__ Key shfl_xor(Key v, int o) {
   return (Key)(unsigned)__shfl_xor((int)(v >> 32), o) << 32 | (unsigned)__shfl_xor((int)(unsigned)v, o);
 }
+
+// Reductions over a wave without a trip through LDS: rotations within rows of 16 lanes, then the swaps of rows and halves.  Every lane gets
+// the result, and the order is the same everywhere.
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+template <class V, class OP>
+__device__ __forceinline__ V rows16(V v, OP op) {
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "one or two registers");
+  auto step = [&](auto c) {
+    if constexpr (sizeof(V) == 4) {
+      v = op(v, __builtin_bit_cast(V, dpp<decltype(c)::value>(__builtin_bit_cast(int, v))));
+    } else {
+      const Key k = __builtin_bit_cast(Key, v);
+      v = op(v, __builtin_bit_cast(V, (Key)(unsigned)dpp<decltype(c)::value>((int)(k >> 32)) << 32 | (unsigned)dpp<decltype(c)::value>((int)(unsigned)k)));
+    }
+  };
+  step(std::integral_constant<int, 0x128>{});   // row_ror 8, 4, 2, 1
+  step(std::integral_constant<int, 0x124>{});
+  step(std::integral_constant<int, 0x122>{});
+  step(std::integral_constant<int, 0x121>{});
+  return v;
+}
+template <class V, class OP>
+__device__ __forceinline__ V wave_all(V v, OP op) {
+  v = rows16(v, op);
+  if constexpr (sizeof(V) == 4) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = op(__builtin_bit_cast(V, (unsigned)p[0]), __builtin_bit_cast(V, (unsigned)p[1]));
+    const unsigned w = __builtin_bit_cast(unsigned, v);
+    const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return op(__builtin_bit_cast(V, (unsigned)q[0]), __builtin_bit_cast(V, (unsigned)q[1]));
+  } else {
+    for (int i = 0; i < 2; ++i) {
+      const Key k = __builtin_bit_cast(Key, v);
+      const unsigned lo = (unsigned)k, hi = (unsigned)(k >> 32);
+      const auto a = i ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+      const auto b = i ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+      v = op(__builtin_bit_cast(V, (Key)(unsigned)b[0] << 32 | (unsigned)a[0]), __builtin_bit_cast(V, (Key)(unsigned)b[1] << 32 | (unsigned)a[1]));
+    }
+    return v;
+  }
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 
 // NT threads that have a row together: 64 (a wave, with the LDS of its own that it is given) or a work-group.  LDS of a group:
 template <int NT>
@@ -62,8 +107,9 @@ struct GroupSpace {
   static constexpr int CANDIDATES = NT == 64 ? 512 : 2048;
   float f[3][16];
   int i[16], n;
-  unsigned i64[64], least;
-  Key waves[16], list[64], next[64], keys[CANDIDATES];
+  unsigned bounds[NT == 64 ? 1 : 256], least;
+  Key waves[16], list[64], next[64];
+  __align__(16) Key keys[CANDIDATES];
 };
 template <int NT>
 struct Group {
@@ -75,9 +121,8 @@ struct Group {
   // over all threads, the same order everywhere; every thread gets the results
   template <int N, class OP>
   __device__ __forceinline__ void reduce(float (&v)[N], OP op) const {
-    for (int o = 1; o < 64; o <<= 1)
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = op(v[k], __shfl_xor(v[k], o));
+    for (int k = 0; k < N; ++k) v[k] = wave_all(v[k], op);
     if (NT == 64) return;
     __syncthreads();
     if ((tid & 63) == 0)
@@ -86,87 +131,99 @@ struct Group {
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      v[k] = sh.f[k][0];
-      for (int w = 1; w < NT / 64; ++w) v[k] = op(v[k], sh.f[k][w]);
+      if constexpr (NT == 1024) v[k] = rows16(sh.f[k][tid & 15], op);
+      else {
+        v[k] = sh.f[k][0];
+#pragma unroll
+        for (int w = 1; w < NT / 64; ++w) v[k] = op(v[k], sh.f[k][w]);
+      }
     }
   }
   __device__ __forceinline__ float max(float v) const {
     float a[1] = {v};
-    reduce(a, [](float x, float y) { return fmaxf(x, y); });
+    reduce(a, larger);
     return a[0];
   }
-  // waves that counted the same number in all their lanes
+  // sum over the waves of a number that all lanes of a wave have
   __device__ __forceinline__ int total(int per_wave) const {
     if (NT == 64) return per_wave;
     __syncthreads();
     if ((tid & 63) == 0) sh.i[tid >> 6] = per_wave;
     __syncthreads();
     int t = 0;
+#pragma unroll
     for (int w = 0; w < NT / 64; ++w) t += sh.i[w];
     return t;
   }
   __device__ __forceinline__ Key max(Key v) const {
-    for (int o = 1; o < 64; o <<= 1) {
-      const Key w = shfl_xor(v, o);
-      v = w > v ? w : v;
-    }
+    v = wave_all(v, [](Key a, Key b) { return a > b ? a : b; });
     if (NT == 64) return v;
     __syncthreads();
     if ((tid & 63) == 0) sh.waves[tid >> 6] = v;
     __syncthreads();
     v = sh.waves[0];
+#pragma unroll
     for (int w = 1; w < NT / 64; ++w) v = sh.waves[w] > v ? sh.waves[w] : v;
     return v;
   }
-  // The `top` largest of everybody's keys, in order, to out(j, key); 0 where there are no more.  mine: the order of this thread's largest
-  // value (0: none); each(f) calls f for all of its keys; at(i), i < n, are all keys once more (0: none), those of equal values in the order
-  // of their classes.  The top-th largest of 64 groups' maxima is a lower bound of the last entry: what is not below it is collected and
-  // ordered by counting.  Where that is too much, thousands of equal logits most likely, only what is above the bound is collected, and of
-  // those at the bound the first; where that is too much still, `top` rounds of maxima decide.
+  // The `top` largest of everybody's keys, in order, to out(j, key); 0 where there are no more.  mine[]: the order of the largest value in each
+  // quarter of what this thread has (0: none; a work-group of more than a wave needs mine[0] alone); each(border, f) calls f for all of its keys of
+  // a value >= border; at(i), i < n, are all keys once more (0: none), those of equal values in the order of their classes.
+  // A number that at least `top` of 256 groups' maxima reach is a lower bound of the last entry, a good one: what is not below it is
+  // collected and ordered by counting.  Where that is too much, thousands of equal logits most likely, only what is above the bound is
+  // collected, and of those at the bound the first; where that is too much still, `top` rounds of maxima decide.
   template <class EACH, class AT, class OUT>
-  __device__ __forceinline__ void select(int top, unsigned mine, EACH each, AT at, int n, OUT out) const {
-    constexpr int LANES = NT / 64;        // per group
-    unsigned g = mine;
-    for (int o = 1; o < LANES; o <<= 1) {
-      const unsigned w = (unsigned)__shfl_xor((int)g, o);
-      g = w > g ? w : g;
+  __device__ __forceinline__ void select(int top, const unsigned (&mine)[4], EACH each, AT at, int n, OUT out) const {
+    constexpr int LANES = NT / 256;       // per group
+    unsigned g[4] = {mine[0], mine[1], mine[2], mine[3]};
+    if (NT > 64) {
+      if (LANES >= 2) { const unsigned w = (unsigned)dpp<0xb1>((int)g[0]); g[0] = w > g[0] ? w : g[0]; }    // quad_perm 1 0 3 2
+      if (LANES >= 4) { const unsigned w = (unsigned)dpp<0x4e>((int)g[0]); g[0] = w > g[0] ? w : g[0]; }    // quad_perm 2 3 0 1
+      __syncthreads();
+      if (tid % (LANES < 1 ? 1 : LANES) == 0) sh.bounds[tid / (LANES < 1 ? 1 : LANES)] = g[0];
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      if (tid < 64) {
+        const uint4 q = *reinterpret_cast<const uint4*>(&sh.bounds[tid * 4]);
+        g[0] = q.x; g[1] = q.y; g[2] = q.z; g[3] = q.w;
+      }
+    } else if (tid == 0) {
+      sh.n = 0;
     }
-    sync();
-    if (tid % LANES == 0) sh.i64[tid / LANES] = g;
-    sync();
+    unsigned least = 0;
     if (tid < 64) {
-      g = sh.i64[tid];
-      int above = 0;                      // equal ones count in the order of the lanes
-      for (int i = 0; i < 64; ++i) {
-        const unsigned o = (unsigned)__builtin_amdgcn_readlane((int)g, i);
-        above += o > g || (o == g && i < tid);
+      for (unsigned bit = 0x80000000u; bit >= 0x2000u; bit >>= 1) {       // 19 bits: as fine as bf16 and three more
+        const unsigned t = least | bit;
+        const int c = __popcll(__ballot(g[0] >= t)) + __popcll(__ballot(g[1] >= t)) + __popcll(__ballot(g[2] >= t)) + __popcll(__ballot(g[3] >= t));
+        if (c >= top) least = t;
+        if (c == top) break;
       }
-      if (above == top - 1) sh.least = g;
+      if (least < LOWEST) least = LOWEST;
+      if (NT > 64 && tid == 0) sh.least = least;
     }
     sync();
-    const unsigned least = sh.least < 1 ? 1 : sh.least;
-    auto collect = [&](Key k, unsigned border) {
-      if ((unsigned)(k >> 32) >= border) {
-        const int i = atomicAdd(&sh.n, 1);
-        if (i < GroupSpace<NT>::CANDIDATES) sh.keys[i] = k;
-      }
+    if (NT > 64) least = sh.least;
+    auto collect = [&](Key k) {
+      const int i = atomicAdd(&sh.n, 1);
+      if (i < GroupSpace<NT>::CANDIDATES) sh.keys[i] = k;
     };
-    if (tid == 0) sh.n = 0;
-    sync();
-    if (mine >= least) each([&](Key k) { collect(k, least); });
+    if (mine[0] >= least || mine[1] >= least || mine[2] >= least || mine[3] >= least) each(value_at(least), collect);
     sync();
     int found = sh.n;
-    if (found > GroupSpace<NT>::CANDIDATES && least != 0xffffffffu) {
+    if (found > GroupSpace<NT>::CANDIDATES) {
       sync();
       if (tid == 0) sh.n = 0;
       sync();
-      for (int i = tid; i < n; i += NT) collect(at(i), least + 1);
+      for (int i = tid; i < n; i += NT) {
+        const Key k = at(i);
+        if ((unsigned)(k >> 32) > least) collect(k);
+      }
       sync();
       found = sh.n;
-      const unsigned border = found <= GroupSpace<NT>::CANDIDATES - 64 ? least : 0;
-      for (int i0 = 0; border && i0 < n && found < top; i0 += NT) {      // the first ones at the bound
+      const bool few = found <= GroupSpace<NT>::CANDIDATES - 64;
+      for (int i0 = 0; few && i0 < n && found < top; i0 += NT) {      // the first ones at the bound
         const Key k = i0 + tid < n ? at(i0 + tid) : 0;
-        const bool is = (unsigned)(k >> 32) == border;
+        const bool is = (unsigned)(k >> 32) == least;
         const unsigned long long lanes = __ballot(is);
         if (NT > 64) {
           __syncthreads();
@@ -190,8 +247,13 @@ struct Group {
     if (found <= GroupSpace<NT>::CANDIDATES) {
       for (int i = tid; i < found; i += NT) {
         const Key k = sh.keys[i];
-        int above = 0;
-        for (int j = 0; j < found; ++j) above += sh.keys[j] > k;
+        int above = 0, j = 0;
+        for (; j + 8 <= found; j += 8) {
+          const ulonglong2* q = reinterpret_cast<const ulonglong2*>(&sh.keys[j]);
+          const ulonglong2 a = q[0], b = q[1], c = q[2], d = q[3];
+          above += (a.x > k) + (a.y > k) + (b.x > k) + (b.y > k) + (c.x > k) + (c.y > k) + (d.x > k) + (d.y > k);
+        }
+        for (; j < found; ++j) above += sh.keys[j] > k;
         if (above < top) out(above, k);
       }
       for (int j = found + tid; j < top; j += NT) out(j, 0);
@@ -266,10 +328,12 @@ struct Held {
       for (int e = 0; e < E; ++e) f(get(j, e), j, e);
     }
   }
-  __device__ __forceinline__ float largest() {
-    float m = -INF;
-    each([&](float s, int, int) { m = fmaxf(m, s); });
-    return m;
+  // largest of the thread's elements; part[]: of the units j with j % 4 == i
+  __device__ __forceinline__ float largest(float (&part)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[i] = -INF;
+    each([&](float s, int j, int) { part[j & 3] = fmaxf(part[j & 3], s); });
+    return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
   }
 };
 
@@ -299,8 +363,7 @@ __device__ __forceinline__ int count_before(H& h, int base, int label, float min
       if (at / E == h.tid + j * H::THREADS)
 #pragma unroll
         for (int e = 0; e < H::E; ++e) more += e < at % E && h.get(j, e) == mine;
-  for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o);
-  return n + more;
+  return n + wave_all(more, [](int a, int b) { return a + b; });
 }
 
 // {m, rest, dot} of what a group holds.  Only waves that hold a maximum keep it apart from the sum.
@@ -334,7 +397,7 @@ __device__ __forceinline__ void write_row(const LogprobForward& a, int row, cons
   const bool broken = v.broken();
   const float lz = v.empty() ? -INF : log1pf(v.rest);
   if (a.logprob)
-    a.logprob[row] = label == -1 ? 0.f : (broken || !has) ? quiet_nan() : v.empty() ? -INF : (float)((double)mine - v.m - log1p((double)v.rest));
+    a.logprob[row] = label == -1 ? 0.f : (broken || !has) ? quiet_nan() : v.empty() ? -INF : (mine - v.m) - lz;   // both terms are <= 0
   if (a.rank) a.rank[row] = has && !broken ? before : -1;
   if (a.entropy) a.entropy[row] = broken ? quiet_nan() : v.empty() ? 0.f : lz - v.dot / (1.f + v.rest);
   if (a.stats) {
@@ -362,40 +425,49 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_logprob_forward(Logprob
   const T* s = (const T*)a.logits + row * a.ld;
   const int label = a.labels ? a.labels[row] : -1;
   const bool has = label >= 0 && label < a.classes;
-  const float mine = has ? to_f32(s[label]) : INF;
   const long c_begin = part * per_part, c_end = c_begin + per_part < a.classes ? c_begin + per_part : a.classes;
   RowSum v = RowSum::none();
+  float mine = INF;
   int before = 0;
   Key held = 0;                                        // entry g.tid of the list of the chunks so far, which is in LDS too
   int kept = 0;
-  long step;
   H h;
-  for (long c0 = c_begin; c0 < c_end; c0 += step) {
-    const long room = H::CAPACITY - (long)(((uintptr_t)(s + c0) & 15) / sizeof(T));
-    step = c_end - c0 < room ? c_end - c0 : room;
+  auto load = [&](long c0) {
+    const long room = H::CAPACITY - (long)(((uintptr_t)(s + c0) & 15) / sizeof(T)), step = c_end - c0 < room ? c_end - c0 : room;
     h.load(s + c0, (int)step, g.tid);
-    const float largest = h.largest();
+    return step;
+  };
+  long step = load(c_begin);
+  if (has) mine = to_f32(s[label]);
+  for (long c0 = c_begin;;) {
+    float quarter[4];
+    const float largest = h.largest(quarter);
     const RowSum w = sum_of(g, h, largest);
     if (c0 == c_begin) v = w; else v.merge(w);
     if (has) before += count_before(h, (int)c0, label, mine, H::E);
-    if (a.top) {
-      unsigned best = (unsigned)(held >> 32);
-      if (largest > -INF && order_of(largest) > best) best = order_of(largest);
-      const bool more = c0 + step < c_end;             // the list goes on, in LDS
-      const bool direct = parts == 1 && !more;
+    const bool more = c0 + step < c_end;
+    if (a.top && !v.broken()) {
+      unsigned best[4] = {0, 0, 0, 0};
+      if (NT == 64) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) best[i] = quarter[i] > -INF ? order_of(quarter[i]) : 0;
+      } else if (largest > -INF) {
+        best[0] = order_of(largest);
+      }
+      if ((unsigned)(held >> 32) > best[0]) best[0] = (unsigned)(held >> 32);
       const float lz = v.empty() ? 0.f : log1pf(v.rest);
 #pragma unroll
       for (int j = 0; j < J; ++j) h.renew(j);
-      g.select(a.top, best, [&](auto f) {
-        if (held) f(held);
-        h.each([&](float t, int j, int e) { if (t > -INF) f(key_of(t, (int)c0 + h.first(j) + e)); }, false);
+      g.select(a.top, best, [&](float border, auto f) {
+        if (held && value_of(held) >= border) f(held);
+        h.each([&](float t, int j, int e) { if (t >= border) f(key_of(t, (int)c0 + h.first(j) + e)); }, false);
       }, [&](int i) -> Key {
-        if (i < a.top) return i < kept ? g.sh.list[i] : 0;           // classes of earlier chunks come first
+        if (i < a.top) return i < kept ? g.sh.list[i] : 0;             // classes of earlier chunks come first
         const float t = to_f32(s[c0 + i - a.top]);
         return t > -INF ? key_of(t, (int)c0 + i - a.top) : 0;
       }, (int)step + a.top, [&](int j, Key k) {
-        if (direct) write_entry(a, row, j, k, v, lz);
-        else if (more) g.sh.next[j] = k;
+        if (more) g.sh.next[j] = k;                                    // the list goes on, in LDS
+        else if (parts == 1) write_entry(a, row, j, k, v, lz);
         else lists[unit * a.top + j] = k;
       });
       if (more) {
@@ -405,7 +477,15 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_logprob_forward(Logprob
         g.sync();
       }
     }
+    if (!more) break;
+    c0 += step;
+    step = load(c0);
   }
+  if (a.top && v.broken())
+    for (int j = g.tid; j < a.top; j += NT) {
+      if (parts == 1) write_entry(a, row, j, 0, v, 0.f);
+      else lists[unit * a.top + j] = 0;
+    }
   before = g.total(before);
   if (g.tid) return;
   if (parts == 1) write_row(a, row, v, before, label, has, mine);
@@ -426,8 +506,8 @@ __global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int part
   if (g.tid < parts) rec[g.tid] = records[(long)row * parts + g.tid];
   const Key* list = lists + (long)row * parts * a.top;
   const int n = parts * a.top;
-  unsigned best = 0;
-  for (int i = g.tid; i < n; i += 256) best = (unsigned)(list[i] >> 32) > best ? (unsigned)(list[i] >> 32) : best;
+  unsigned best[4] = {0, 0, 0, 0};
+  for (int i = g.tid; i < n; i += 256) best[0] = (unsigned)(list[i] >> 32) > best[0] ? (unsigned)(list[i] >> 32) : best[0];
   __syncthreads();
   RowSum v = RowSum::none();
   int before = 0;
@@ -435,7 +515,7 @@ __global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int part
   if (g.tid == 0) write_row(a, row, v, before, label, has, mine);
   if (!a.top) return;
   const float lz = v.empty() ? 0.f : log1pf(v.rest);
-  g.select(a.top, best, [&](auto f) { for (int i = g.tid; i < n; i += 256) if (list[i]) f(list[i]); },
+  g.select(a.top, best, [&](float border, auto f) { for (int i = g.tid; i < n; i += 256) if (list[i] && value_of(list[i]) >= border) f(list[i]); },
            [&](int i) { return list[i]; }, n, [&](int j, Key k) { write_entry(a, row, j, k, v, lz); });
 }
 
@@ -448,17 +528,20 @@ __global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a, uns
   const int b = (int)(blockIdx.x - (unsigned)row * blocks_per_row);
   const T* s = (const T*)a.logits + row * a.ld;
   T* d = (T*)a.dlogits + row * a.ldd;
-  const int label = a.labels ? a.labels[row] : -1;
+  const int label = a.grad_logprob ? a.labels[row] : -1;
   const float m = a.stats[2 * (long)row], lz = a.stats[2 * (long)row + 1];
-  float g = a.grad_logprob && label != -1 ? a.grad_logprob[row] : 0.f;
+  float g = label != -1 ? a.grad_logprob[row] : 0.f;
   if (label < -1 || label >= a.classes) g = quiet_nan();
   const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.f, h = a.grad_entropy ? a.entropy[row] : 0.f;
-  auto grad = [&](float x, int c) {
+  const float ng = -g, ngh = -gh;
+  auto grad = [&](float x) {
     const float logp = (x - m) - lz, p = __builtin_amdgcn_exp2f(logp * LOG2E);
-    // p = 0: the class is masked or as good as that; its entropy term is p log p -> 0
-    float v = fmaf(-gh * p, fmaxf(logp, -3e38f) + h, -g * p);
-    if (c == label) v = fmaf(-gh * p, fmaxf(logp, -3e38f) + h, -g * expm1f(logp));
-    return m == -INF ? 0.f : v;
+    // p is 0 below exp(-104), in a masked class for one, and the entropy's p log p with it
+    return m == -INF ? 0.f : p * fmaf(ngh, fmaxf(logp, -120.f) + h, ng);
+  };
+  auto grad_label = [&](float x) {             // 1 - p from log p
+    const float logp = (x - m) - lz, p = __builtin_amdgcn_exp2f(logp * LOG2E);
+    return m == -INF ? 0.f : fmaf(ngh * p, fmaxf(logp, -120.f) + h, ng * expm1f(logp));
   };
   const int shift = (int)(((uintptr_t)s & 15) / sizeof(T));
   const bool alike = (((uintptr_t)s ^ (uintptr_t)d) & 15) == 0;
@@ -467,30 +550,33 @@ __global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a, uns
     const long e0 = ((long)b * (256 * U) + u * 256 + threadIdx.x) * E - shift;
     if (e0 >= a.classes) break;
     if (alike && e0 >= 0 && e0 + E <= a.classes) {
-      float x[8];
-      if (sizeof(T) == 2) {
+      float x[E], y[E];
+      if constexpr (sizeof(T) == 2) {
         load8((const bf16_t*)s + e0, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = grad(x[e], (int)e0 + e);
-        store8((bf16_t*)d + e0, x);
       } else {
-        float4 q = *reinterpret_cast<const float4*>((const float*)s + e0);
-        q = make_float4(grad(q.x, (int)e0), grad(q.y, (int)e0 + 1), grad(q.z, (int)e0 + 2), grad(q.w, (int)e0 + 3));
-        *reinterpret_cast<float4*>((float*)d + e0) = q;
+        const float4 q = *reinterpret_cast<const float4*>((const float*)s + e0);
+        x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
       }
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = grad(x[e]);
+      if (label >= e0 && label < e0 + E)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e0 + e == label) y[e] = grad_label(x[e]);
+      if constexpr (sizeof(T) == 2) store8((bf16_t*)d + e0, y);
+      else *reinterpret_cast<float4*>((float*)d + e0) = make_float4(y[0], y[1], y[2], y[3]);
     } else {
       for (int e = 0; e < E; ++e)
-        if (e0 + e >= 0 && e0 + e < a.classes) from_f32(d + e0 + e, grad(to_f32(s[e0 + e]), (int)e0 + e));
+        if (e0 + e >= 0 && e0 + e < a.classes) {
+          const float x = to_f32(s[e0 + e]);
+          from_f32(d + e0 + e, e0 + e == label ? grad_label(x) : grad(x));
+        }
     }
   }
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------
-// sums over the wave, in double; every lane gets the result
-__device__ __forceinline__ double wave_sum(double v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
+__device__ __forceinline__ double wave_sum(double v) { return wave_all(v, [](double a, double b) { return a + b; }); }
 
 // What the student's row leaves for the loss: the maximum and the sums of the other classes at temperature 1 and T
 struct Soft { float m, rest1, restt; };
@@ -509,54 +595,76 @@ __device__ __forceinline__ void merge(Soft& v, const Soft& o, float it) {
 struct List {
   bool on, some, broken;     // entry there; any entry there; an index outside the classes
   int index;
+  float mine;                // the student's logit at the entry's class
+  double p, logp;            // probability of the entry
   double soft;               // sum_j p_j (log p_j - log q_j)
   double diff;               // q_c - P_c, P_c: probability of the entry's class in the list (all entries of that class)
 };
+// what does not need the row's sums
 template <class T>
-__device__ __forceinline__ List read_list(const Distill& a, const T* s, int row, const Soft& v, int lane) {
+__device__ __forceinline__ List read_list(const Distill& a, const T* s, int row, int lane) {
   List l{};
   const long at = (long)row * a.top + lane;
   l.index = lane < a.top ? a.top_index[at] : -1;
-  const double t = l.index >= 0 ? (double)a.top_logit[at] : -(double)INF;
-  l.on = t != -(double)INF;
+  const float t = l.index >= 0 ? a.top_logit[at] : -INF;
+  l.on = t != -INF;
   l.broken = __any(l.on && l.index >= a.classes);
   l.some = __any(l.on);
-  const bool in = l.on && l.index < a.classes;
-  const double it = 1.0 / (double)a.temperature;
-  double top = t;
-  for (int o = 32; o > 0; o >>= 1) { const double u = __shfl_xor(top, o); top = u > top ? u : top; }
-  const double e = l.on ? exp((t - top) * it) : 0.0;
-  const double z = wave_sum(e);
-  const double p = e / z;
-  const double logp = (t - top) * it - log(z);
-  const double logq = in ? ((double)to_f32(s[l.index]) - v.m) * it - log1p((double)v.restt) : 0.0;
-  l.soft = wave_sum(l.on && p != 0.0 ? p * (logp - logq) : 0.0);
-  double same = 0.0;
-  for (int j = 0; j < a.top; ++j) {
-    const double pj = __shfl(p, j);
-    if (__shfl(l.index, j) == l.index) same += pj;
-  }
-  l.diff = same != 0.0 ? same * expm1(logq - log(same)) : exp(logq);
+  l.mine = l.on && l.index < a.classes ? to_f32(s[l.index]) : 0.f;
+  if (!l.some) return l;
+  const double d = ((double)t - (double)wave_all(t, larger)) / (double)a.temperature;
+  const double e = l.on ? exp(d) : 0.0, z = wave_sum(e);
+  l.p = e / z;
+  l.logp = d - log(z);
   return l;
+}
+__device__ __forceinline__ void finish_list(const Distill& a, List& l, const Soft& v) {
+  if (!l.some) return;
+  const double logq = l.on ? ((double)l.mine - (double)v.m) / (double)a.temperature - log1p((double)v.restt) : 0.0;
+  l.soft = wave_sum(l.on && l.p != 0.0 ? l.p * (l.logp - logq) : 0.0);
+  int same = 0;              // entries of this lane's class
+  for (int j = 0; j < a.top; ++j) same += __builtin_amdgcn_readlane(l.index, j) == l.index;
+  double p = l.p, logp = l.logp;
+  if (__any(l.on && same > 1)) {
+    p = 0.0;
+    for (int j = 0; j < a.top; ++j) {
+      const double pj = __shfl(l.p, j);
+      if (__builtin_amdgcn_readlane(l.index, j) == l.index) p += pj;
+    }
+    logp = log(p);
+  }
+  l.diff = p != 0.0 ? p * expm1(logq - logp) : exp(logq);
+}
+
+// exp at temperature 1 next to exp at temperature T: HARD_EXP of its own, or HARD_ONE / HARD_TWO / HARD_FOUR: e^(1/T) to the power T = 1, 2, 4
+// (an exponential costs four times a multiplication)
+enum : int { HARD_NONE = 0, HARD_EXP = 1, HARD_ONE = 2, HARD_TWO = 3, HARD_FOUR = 4 };
+template <int HARD>
+__device__ __forceinline__ float hard_exp(float d, float et) {
+  if (HARD == HARD_ONE) return et;
+  if (HARD == HARD_TWO) return et * et;
+  if (HARD == HARD_FOUR) { const float q = et * et; return q * q; }
+  return __builtin_amdgcn_exp2f(d * LOG2E);
 }
 
 // Sums of what a group holds at temperatures 1 (if HARD) and T
-template <bool HARD, class T, int NT, int J>
+template <int HARD, class T, int NT, int J>
 __device__ __forceinline__ Soft soft_of(const Group<NT>& g, Held<T, NT, J>& h, float it) {
-  const float largest = h.largest(), m = g.max(largest), mm = m == -INF ? 0.f : m, ct = LOG2E * it;
+  float quarter[4];
+  const float largest = h.largest(quarter), m = g.max(largest), mm = m == -INF ? 0.f : m, ct = LOG2E * it;
   float v[3] = {0.f, 0.f, 0.f};                // rest at T, rest at 1, classes at the maximum
   if (NT == 64 || __any(largest == m)) {
     h.each([&](float s, int, int) {
-      const float d = s - mm;
-      v[0] += d == 0.f ? 0.f : __builtin_amdgcn_exp2f(d * ct);
-      if (HARD) v[1] += d == 0.f ? 0.f : __builtin_amdgcn_exp2f(d * LOG2E);
+      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * ct);
+      v[0] += d == 0.f ? 0.f : e;
+      if (HARD) v[1] += d == 0.f ? 0.f : hard_exp<HARD>(d, e);
       v[2] += d == 0.f ? 1.f : 0.f;
     });
   } else {
     h.each([&](float s, int, int) {
-      const float d = s - mm;
-      v[0] += __builtin_amdgcn_exp2f(d * ct);
-      if (HARD) v[1] += __builtin_amdgcn_exp2f(d * LOG2E);
+      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * ct);
+      v[0] += e;
+      if (HARD) v[1] += hard_exp<HARD>(d, e);
     });
   }
   g.reduce(v, [](float a, float b) { return a + b; });
@@ -571,18 +679,25 @@ struct Answer {
   const T* s;
   int row, label;
   bool has, bad, empty;
+  float mine;                // logit of the label
   double logl, ws, wh;       // log softmax at the label; weights of the soft and the hard term
-  float fs, fh;              // the same over Z
+  float fs, fh, weight;      // the same over Z; the row's weight
   Soft v;
 
-  __device__ __forceinline__ Answer(const Distill& a_, const T* s_, int row_, const Soft& v_, bool some, bool list_broken) : a(a_), s(s_), row(row_), v(v_) {
+  // what does not need the row's sums: loads that are on their way with the row
+  __device__ __forceinline__ Answer(const Distill& a_, const T* s_, int row_) : a(a_), s(s_), row(row_) {
     label = a.labels ? a.labels[row] : -1;
     has = label >= 0 && label < a.classes;
+    weight = a.row_weight ? a.row_weight[row] : 1.f;
+    mine = has ? to_f32(s[label]) : 0.f;
+  }
+  __device__ __forceinline__ void finish(const Soft& v_, bool some, bool list_broken) {
+    v = v_;
     const bool hard = a.hard_weight != 0.f;
     empty = v.m == -INF;
     bad = v.m == INF || v.restt != v.restt || (hard && v.rest1 != v.rest1) || list_broken || (label != -1 && !has);
-    const double hw = (double)a.hard_weight, w = a.row_weight ? (double)a.row_weight[row] : 1.0;
-    logl = has && hard ? (double)to_f32(s[label]) - v.m - log1p((double)v.rest1) : 0.0;
+    const double hw = (double)a.hard_weight, w = (double)weight;
+    logl = has && hard ? (double)mine - (double)v.m - log1p((double)v.rest1) : 0.0;
     ws = some ? w * (1.0 - hw) * a.temperature : 0.0;
     wh = has ? w * hw : 0.0;
     fs = bad ? quiet_nan() : (float)(ws / (1.0 + v.restt));
@@ -598,22 +713,20 @@ struct Answer {
   // the gradient at the listed classes and the label, where q - p and p - 1 may cancel, among classes [c0, c1); by one wave
   __device__ __forceinline__ void write_entries(const List& l, T* d, long c0, long c1, int lane) const {
     if (bad || empty) return;
-    const double it = 1.0 / (double)a.temperature;
     const bool listed = __any(l.on && l.index == label);
     if (l.on && l.index >= c0 && l.index < c1) {
-      const double t = (double)to_f32(s[l.index]) - v.m;
-      const double hard = wh == 0.0 ? 0.0 : l.index == label ? expm1(logl) : exp(t - log1p((double)v.rest1));
+      const double hard = wh == 0.0 ? 0.0 : l.index == label ? expm1(logl) : (double)expf(l.mine - v.m) / (1.0 + (double)v.rest1);
       from_f32(d + l.index, (float)(ws * l.diff + wh * hard));
     }
     if (has && !listed && label >= c0 && label < c1 && lane == 0) {
-      const double q = exp(((double)to_f32(s[label]) - v.m) * it - log1p((double)v.restt));
+      const double q = (double)expf((mine - v.m) * (1.f / a.temperature)) / (1.0 + (double)v.restt);
       from_f32(d + label, (float)(ws * q + wh * expm1(logl)));
     }
   }
 };
 
 // gradient of the `len` held elements to d
-template <bool HARD, class T, int NT, int J>
+template <int HARD, class T, int NT, int J>
 __device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero) {
   typedef Held<T, NT, J> H;
   const float ct = LOG2E * it;
@@ -625,9 +738,9 @@ __device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m,
     float x[H::E];
 #pragma unroll
     for (int e = 0; e < H::E; ++e) {
-      const float t = h.get(j, e) - m;
-      x[e] = fs * __builtin_amdgcn_exp2f(t * ct);
-      if (HARD) x[e] = fmaf(fh, __builtin_amdgcn_exp2f(t * LOG2E), x[e]);
+      const float t = h.get(j, e) - m, et = __builtin_amdgcn_exp2f(t * ct);
+      x[e] = fs * et;
+      if (HARD) x[e] = fmaf(fh, hard_exp<HARD>(t, et), x[e]);
       if (zero) x[e] = 0.f;
     }
     const int e0 = h.first(j);
@@ -649,7 +762,7 @@ __device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m,
 }
 
 // a row that a group holds whole
-template <bool HARD, class T, int NT, int J>
+template <int HARD, class T, int NT, int J>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill(Distill a) {
   constexpr int PER = NT < 256 ? 256 / NT : 1;
   __shared__ GroupSpace<NT> space[PER];
@@ -660,20 +773,20 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill(Distill a) {
   const float it = 1.f / a.temperature;
   Held<T, NT, J> h;
   h.load(s, a.classes, g.tid);
-  const Soft v = soft_of<HARD>(g, h, it);
-  // every wave needs to know whether the list has entries and bad ones; the first one reads it
+  Answer<T> ans(a, s, row);
   List l{};
-  if (g.tid < 64) {
-    l = read_list(a, s, row, v, g.tid);
-    if (NT > 64 && g.tid == 0) g.sh.n = (int)l.some | (int)l.broken << 1;
-  }
+  if (g.tid < 64) l = read_list(a, s, row, g.tid);
+  const Soft v = soft_of<HARD>(g, h, it);
+  // every wave needs to know whether the list has entries and bad ones; the first one has read it
   bool some = l.some, broken = l.broken;
   if (NT > 64) {
+    if (g.tid == 0) g.sh.n = (int)l.some | (int)l.broken << 1;
     __syncthreads();
     some = g.sh.n & 1;
     broken = g.sh.n & 2;
   }
-  const Answer<T> ans(a, s, row, v, some, broken);
+  ans.finish(v, some, broken);
+  if (g.tid < 64) finish_list(a, l, v);
   if (g.tid == 0) ans.write_loss(l);
   if (!a.dlogits) return;
   T* d = (T*)a.dlogits + row * a.ldd;
@@ -683,7 +796,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill(Distill a) {
 }
 
 // a row divided among work-groups: first their sums ...
-template <bool HARD, class T, int J>
+template <int HARD, class T, int J>
 __global__ __launch_bounds__(256) void k_distill_part(Distill a, int parts, long per_part, Soft* records) {
   typedef Held<T, 256, J> H;
   __shared__ GroupSpace<256> space;
@@ -705,7 +818,7 @@ __global__ __launch_bounds__(256) void k_distill_part(Distill a, int parts, long
   if (g.tid == 0) records[blockIdx.x] = v;
 }
 // ... then loss and gradient
-template <bool HARD, class T, int J>
+template <int HARD, class T, int J>
 __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long per_part, const Soft* __restrict__ records) {
   typedef Held<T, 256, J> H;
   __shared__ Soft rec[256];
@@ -716,8 +829,10 @@ __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long
   __syncthreads();
   Soft v = rec[0];
   for (int i = 1; i < parts; ++i) merge(v, rec[i], it);
-  const List l = read_list(a, s, row, v, tid & 63);
-  const Answer<T> ans(a, s, row, v, l.some, l.broken);
+  List l = read_list(a, s, row, tid & 63);
+  finish_list(a, l, v);
+  Answer<T> ans(a, s, row);
+  ans.finish(v, l.some, l.broken);
   if (part == 0 && tid == 0) ans.write_loss(l);
   if (!a.dlogits) return;
   T* d = (T*)a.dlogits + row * a.ldd;
@@ -780,7 +895,7 @@ hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hip
     k_logprob_join<T><<<(unsigned)a.rows, 256, 0, s>>>(a, c.parts, records, lists);
   } else if (c.units <= 64 * 4) k_logprob_forward<T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
   else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
-  else if (c.units <= 1024 * 8) k_logprob_forward<T, 1024, 8><<<(unsigned)a.rows, 1024, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
+  else if (c.units <= 512 * 16) k_logprob_forward<T, 512, 16><<<(unsigned)a.rows, 512, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
   else k_logprob_forward<T, 1024, 16><<<(unsigned)a.rows, 1024, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
   return hipGetLastError();
 }
@@ -793,21 +908,31 @@ hipError_t logprob_backward(const LogprobBackward& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool HARD, class T>
-hipError_t distill(int dt, const Distill& a, void* workspace, hipStream_t s) {
+template <int HARD, class T>
+hipError_t distill_as(int dt, const Distill& a, void* workspace, hipStream_t s) {
   const RowCut c = row_cut(dt, a.rows, a.classes, aligned16(a.logits, a.ld, sizeof(T)));
   if (c.parts > 1) {
     const unsigned n = (unsigned)((long)a.rows * c.parts);
     Soft* records = (Soft*)workspace;
-    k_distill_part<HARD, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
+    constexpr int ANY = HARD ? HARD_EXP : HARD_NONE;
+    k_distill_part<ANY, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_distill_join<HARD, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
-  } else if (c.units <= 64 * 4) k_distill<HARD, T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
+    k_distill_join<ANY, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
+  } else if (c.units <= 64 * 4) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
   else if (c.units <= 256 * 8) k_distill<HARD, T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
-  else if (c.units <= 1024 * 8) k_distill<HARD, T, 1024, 8><<<(unsigned)a.rows, 1024, 0, s>>>(a);
+  else if (c.units <= 512 * 16) k_distill<HARD, T, 512, 16><<<(unsigned)a.rows, 512, 0, s>>>(a);
   else k_distill<HARD, T, 1024, 16><<<(unsigned)a.rows, 1024, 0, s>>>(a);
   return hipGetLastError();
+}
+
+template <class T>
+hipError_t distill(int dt, const Distill& a, void* workspace, hipStream_t s) {
+  if (a.hard_weight == 0.f) return distill_as<HARD_NONE, T>(dt, a, workspace, s);
+  if (a.temperature == 1.f) return distill_as<HARD_ONE, T>(dt, a, workspace, s);
+  if (a.temperature == 2.f) return distill_as<HARD_TWO, T>(dt, a, workspace, s);
+  if (a.temperature == 4.f) return distill_as<HARD_FOUR, T>(dt, a, workspace, s);
+  return distill_as<HARD_EXP, T>(dt, a, workspace, s);
 }
 
 }  // namespace
@@ -825,9 +950,7 @@ hipError_t launch_logprob_backward(int dt, const LogprobBackward& a, hipStream_t
   return dt == DT_BF16 ? logprob_backward<bf16_t>(a, stream) : logprob_backward<float>(a, stream);
 }
 hipError_t launch_distill(int dt, const Distill& a, void* workspace, hipStream_t stream) {
-  const bool hard = a.hard_weight != 0.f;
-  if (dt == DT_BF16) return hard ? distill<true, bf16_t>(dt, a, workspace, stream) : distill<false, bf16_t>(dt, a, workspace, stream);
-  return hard ? distill<true, float>(dt, a, workspace, stream) : distill<false, float>(dt, a, workspace, stream);
+  return dt == DT_BF16 ? distill<bf16_t>(dt, a, workspace, stream) : distill<float>(dt, a, workspace, stream);
 }
 
 }  // namespace hpf
