@@ -274,7 +274,8 @@ struct Group {
 };
 
 // `len` elements from p on, held by NT threads as they are stored: unit j of thread t is 16-byte unit t + j * NT, counted from the 16-byte
-// boundary at or before p.  Elements before p or behind the end read as -infinity; units that lie across an end are read element by element.
+// boundary at or before p.  Elements before p or behind the end read as -infinity.  Only the first and the last unit can lie across an end;
+// these two are read and written element by element.
 template <class T, int NT, int J>
 struct Held {
   static constexpr int E = 16 / sizeof(T), CAPACITY = NT * J * E, UNITS = J, THREADS = NT;
@@ -283,47 +284,106 @@ struct Held {
 
   __device__ __forceinline__ bool used(int j) const { return j * NT * E - shift < len; }      // uniform
   __device__ __forceinline__ int first(int j) const { return (tid + j * NT) * E - shift; }
-  __device__ __forceinline__ bool inside(int j) const { const int e0 = first(j); return e0 >= 0 && e0 + E <= len; }
+  __device__ __forceinline__ bool inside(int j) const { const int u = tid + j * NT; return u >= (shift ? 1 : 0) && u < (shift + len) / E; }
 
-  __device__ __forceinline__ void load(const T* p, int n, int t) {
+  // The units j < AHEAD of a row on their way to LDS, past the registers: each thread's own 16 bytes of `room` (NT * AHEAD units)
+  template <int AHEAD>
+  static __device__ __forceinline__ void fetch(const T* p, int n, int t, uint4* room) {
+    const int shift = (int)(((uintptr_t)p & 15) / sizeof(T)), whole = (shift + n) / E, low = shift ? 1 : 0;
+    const char* units = (const char*)(p - shift);      // uniform; a thread's offset is the same for every j
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (j * NT * E - shift >= n) break;
+      if (t + j * NT >= low && t + j * NT < whole)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(units + j * (NT * 16) + (unsigned)t * 16u),
+                                         (__attribute__((address_space(3))) void*)(room + j * NT + (t & ~63)), 16, 0, 0);
+    }
+  }
+  // AHEAD units per thread come from `room`, where fetch has brought them
+  template <int AHEAD = 0>
+  __device__ __forceinline__ void load(const T* p, int n, int t, const uint4* room = nullptr) {
     shift = (int)(((uintptr_t)p & 15) / sizeof(T));
     len = n;
     tid = t;
+    constexpr uint32_t NONE = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    const char* units = (const char*)(p - shift);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       if (!used(j)) break;
-      const int e0 = first(j);
-      if (inside(j)) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p + e0);
-        v[j][0] = q.x; v[j][1] = q.y; v[j][2] = q.z; v[j][3] = q.w;
-      } else {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) v[j][w] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-        if (e0 < len)
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (e0 + e >= 0 && e0 + e < len) set(j, e, p[e0 + e]);
-      }
+      uint4 q = make_uint4(NONE, NONE, NONE, NONE);
+      if (inside(j)) q = j < AHEAD ? room[t + j * NT] : *reinterpret_cast<const uint4*>(units + j * (NT * 16) + (unsigned)t * 16u);
+      v[j][0] = q.x; v[j][1] = q.y; v[j][2] = q.z; v[j][3] = q.w;
     }
+    const int whole = (shift + n) / E;
+    if (shift) edge(p, 0, NONE);
+    if ((shift + n) % E && whole >= (shift ? 1 : 0)) edge(p, whole, NONE);
   }
-  __device__ __forceinline__ void set(int j, int e, bf16_t x) { v[j][e >> 1] = e & 1 ? (v[j][e >> 1] & 0xffffu) | (uint32_t)x << 16 : (v[j][e >> 1] & 0xffff0000u) | x; }
-  __device__ __forceinline__ void set(int j, int e, float x) { v[j][e] = __float_as_uint(x); }
+  // unit u lies across an end of the row
+  __device__ __forceinline__ void edge(const T* p, int u, uint32_t none) {
+    uint32_t w[4] = {none, none, none, none};
+    if (u % NT == tid)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = u * E - shift + e;
+        if (i >= 0 && i < len) {
+          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(p[i]);
+          else w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | (uint32_t)p[i] << 16 : (w[e >> 1] & 0xffff0000u) | p[i];
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (u / NT == j && u % NT == tid) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = w[i];
+      }
+  }
   __device__ __forceinline__ float get(int j, int e) const {
     if (sizeof(T) == 4) return __uint_as_float(v[j][e]);
     return __uint_as_float(e & 1 ? v[j][e >> 1] & 0xffff0000u : v[j][e >> 1] << 16);
   }
-  // A pass converts what is stored again: without this the compiler keeps the fp32 values of one pass for the next, twice the registers
-  __device__ __forceinline__ void renew(int j) {
+  // Before a pass that converts what is stored again: without it the compiler keeps the fp32 values of one pass for the next, twice the registers
+  __device__ __forceinline__ void renew() {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) asm("" : "+v"(v[j][w]));
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) asm("" : "+v"(v[j][w]));
   }
-  // f(value, j, e) for all units in use
+  // Every element's f(value, j, e) to the same element of d.  Where d's elements do not have the same places within 16 bytes they are stored
+  // one by one.
   template <class F>
-  __device__ __forceinline__ void each(F f, bool fresh = true) {
+  __device__ __forceinline__ void store(T* d, F f) {
+    const bool alike = (int)(((uintptr_t)d & 15) / sizeof(T)) == shift;
+    const int whole = (shift + len) / E;
+    char* units = (char*)(d - shift);
+    float x[E];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       if (!used(j)) break;
-      if (fresh) renew(j);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = f(get(j, e), j, e);
+      T* at = (T*)(units + j * (NT * 16) + (unsigned)tid * 16u);
+      if (inside(j)) {
+        if (alike) {
+          if constexpr (sizeof(T) == 2) store8((bf16_t*)at, x);
+          else *reinterpret_cast<float4*>(at) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) from_f32(at + e, x[e]);
+        }
+      } else if (j == 0 || whole / NT == j) {
+        const int e0 = first(j);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e0 + e >= 0 && e0 + e < len) from_f32(at + e, x[e]);
+      }
+    }
+  }
+  // f(value, j, e) for all units in use
+  template <class F>
+  __device__ __forceinline__ void each(F f) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (!used(j)) break;
 #pragma unroll
       for (int e = 0; e < E; ++e) f(get(j, e), j, e);
     }
@@ -340,44 +400,51 @@ struct Held {
 // How many classes are before `label`, whose logit is `mine`: larger ones, and equal ones of lower index.  base: class of p's first element.
 // Counted per wave, one comparison per element: units before the label's take the next smaller number as their border.
 template <class H>
-__device__ __forceinline__ int count_before(H& h, int base, int label, float mine, int E) {
+__device__ __forceinline__ int count_before(H& h, int base, int label, float mine) {
+  constexpr int E = H::E;
   int n = 0;
+  h.renew();
+  if (mine == -INF) {                          // a masked label, for which there is no smaller number
+    h.each([&](float s, int j, int e) {
+      const int c = h.first(j) + e;
+      n += __popcll(__ballot(s > mine || (s == mine && c >= 0 && c < h.len && base + c < label)));
+    });
+    return n;
+  }
   const unsigned b = __float_as_uint(mine);
-  const bool exact = mine == -INF;             // a masked label, for which there is no smaller number
   const float below = mine == 0.f ? -__uint_as_float(1) : __uint_as_float(mine > 0.f ? b - 1 : b + 1);
   float border = 0.f;
   h.each([&](float s, int j, int e) {
-    const int e0 = h.first(j);
-    if (e == 0) border = base + e0 + E <= label ? below : mine;
-    bool is = s > border;
-    if (exact) is = s > mine || (s == mine && e0 + e >= 0 && e0 + e < h.len && base + e0 + e < label);
-    n += __popcll(__ballot(is));
+    if (e == 0) border = base + h.first(j) + E <= label ? below : mine;
+    n += __popcll(__ballot(s > border));
   });
-  if (exact) return n;
   // the label's own unit: equal logits in front of it, counted by the thread that holds it
   const int at = label - base + h.shift;       // counted from the first unit's start
-  int more = 0;
-  if (at >= 0 && label - base < h.len)
+  if (label < base || label - base >= h.len) return n;
+  const int unit = at / E, uj = unit / H::THREADS, ut = unit % H::THREADS;
 #pragma unroll
-    for (int j = 0; j < H::UNITS; ++j)
-      if (at / E == h.tid + j * H::THREADS)
+  for (int j = 0; j < H::UNITS; ++j)
+    if (uj == j)
 #pragma unroll
-        for (int e = 0; e < H::E; ++e) more += e < at % E && h.get(j, e) == mine;
-  return n + wave_all(more, [](int a, int b) { return a + b; });
+      for (int e = 0; e < E; ++e) n += __popcll(__ballot(h.tid == ut && e < at % E && h.get(j, e) == mine));
+  return n;
 }
 
 // {m, rest, dot} of what a group holds.  Only waves that hold a maximum keep it apart from the sum.
 template <class T, int NT, int J>
 __device__ __forceinline__ RowSum sum_of(const Group<NT>& g, Held<T, NT, J>& h, float largest) {
   const float m = g.max(largest), mm = m == -INF ? 0.f : m;
+  h.renew();
   float v[3] = {0.f, 0.f, 0.f};                // rest, dot, classes at the maximum
   if (NT == 64 || __any(largest == m)) {
+    int ties = 0;
     h.each([&](float s, int, int) {
       const float d = s - mm, e = __builtin_amdgcn_exp2f(d * LOG2E);
       v[0] += d == 0.f ? 0.f : e;
       v[1] = fmaf(e, fmaxf(d, -3e38f), v[1]);
-      v[2] += d == 0.f ? 1.f : 0.f;
+      ties += __popcll(__ballot(d == 0.f));
     });
+    v[2] = (g.tid & 63) == 0 ? (float)ties : 0.f;
   } else {
     h.each([&](float s, int, int) {
       const float d = s - mm, e = __builtin_amdgcn_exp2f(d * LOG2E);
@@ -412,18 +479,102 @@ __device__ __forceinline__ void write_entry(const LogprobForward& a, int row, in
   a.top_logprob[at] = broken ? quiet_nan() : k ? (value_of(k) - v.m) - lz : -INF;
 }
 
-// Group `part` of `parts` of a row takes every chunk of CAPACITY elements from part * per_part on
+// the order of the largest value in each quarter of what a thread holds
+template <int NT>
+__device__ __forceinline__ void orders(unsigned (&best)[4], const float (&quarter)[4], float largest) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) best[i] = 0;
+  if (NT == 64) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) best[i] = quarter[i] > -INF ? order_of(quarter[i]) : 0;
+  } else if (largest > -INF) {
+    best[0] = order_of(largest);
+  }
+}
+
+// A row that a group holds whole.  s, label and mine are the same in all lanes.
 template <class T, int NT, int J>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_logprob_forward(LogprobForward a, int parts, long per_part, PartRecord* records, Key* lists) {
-  typedef Held<T, NT, J> H;
-  constexpr int PER = NT < 256 ? 256 / NT : 1;         // rows per work-group
+__device__ __forceinline__ void logprob_row(const LogprobForward& a, const Group<NT>& g, Held<T, NT, J>& h, const T* s, int row, int label, float mine) {
+  const bool has = label >= 0 && label < a.classes;
+  float quarter[4];
+  const float largest = h.largest(quarter);
+  const RowSum v = sum_of(g, h, largest);
+  int before = 0;
+  if (has) before = g.total(count_before(h, 0, label, mine));
+  if (g.tid == 0) write_row(a, row, v, before, label, has, mine);
+  if (!a.top) return;
+  if (v.broken()) {
+    for (int j = g.tid; j < a.top; j += NT) write_entry(a, row, j, 0, v, 0.f);
+    return;
+  }
+  unsigned best[4];
+  orders<NT>(best, quarter, largest);
+  const float lz = v.empty() ? 0.f : log1pf(v.rest);
+  h.renew();
+  g.select(a.top, best, [&](float border, auto f) {
+    h.each([&](float t, int j, int e) { if (t >= border) f(key_of(t, h.first(j) + e)); });
+  }, [&](int i) -> Key {
+    const float t = to_f32(s[i]);
+    return t > -INF ? key_of(t, i) : 0;
+  }, a.classes, [&](int j, Key k) { write_entry(a, row, j, k, v, lz); });
+}
+
+__device__ __forceinline__ int label_of(const int* labels, int row) { return labels ? __builtin_amdgcn_readfirstlane(labels[row]) : -1; }
+template <class T>
+__device__ __forceinline__ float logit_of(const T* s, int label, int classes) {
+  return label >= 0 && label < classes ? __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(to_f32(s[label])))) : INF;
+}
+
+// rows that a wave or 256 threads hold: many of them on a CU at a time
+template <class T, int NT, int J>
+__global__ __launch_bounds__(256) void k_logprob_forward(LogprobForward a) {
+  constexpr int PER = 256 / NT;                        // rows per work-group
   __shared__ GroupSpace<NT> space[PER];
-  const Group<NT> g{space[threadIdx.x / NT], (int)threadIdx.x % NT};
-  const long unit = (long)blockIdx.x * PER + threadIdx.x / NT;
-  const int row = (int)(unit / parts), part = (int)(unit - (long)row * parts);
+  const int which = NT == 256 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
+  const Group<NT> g{space[which], (int)threadIdx.x % NT};
+  const int row = blockIdx.x * PER + which;
   if (row >= a.rows) return;                           // a whole wave, or nobody
   const T* s = (const T*)a.logits + row * a.ld;
-  const int label = a.labels ? a.labels[row] : -1;
+  Held<T, NT, J> h;
+  h.load(s, a.classes, g.tid);
+  const int label = label_of(a.labels, row);
+  logprob_row(a, g, h, s, row, label, logit_of(s, label, a.classes));
+}
+
+// Long rows: one work-group per CU goes through rows one after the other.  While it works on one row in registers the next one is on its way to
+// LDS (AHEAD units per thread), so that memory does not wait for the passes.
+template <class T, int J, int AHEAD>
+__global__ __launch_bounds__(1024) void k_logprob_rows(LogprobForward a) {
+  typedef Held<T, 1024, J> H;
+  __shared__ GroupSpace<1024> space;
+  extern __shared__ __align__(16) uint4 room[];
+  const Group<1024> g{space, (int)threadIdx.x};
+  int row = blockIdx.x;
+  const T* s = (const T*)a.logits + row * a.ld;
+  H::template fetch<AHEAD>(s, a.classes, g.tid, room);
+  for (; row < a.rows; row += gridDim.x) {
+    s = (const T*)a.logits + row * a.ld;
+    H h;
+    __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the thread's units are in LDS
+    h.template load<AHEAD>(s, a.classes, g.tid, room);
+    const int label = label_of(a.labels, row);
+    const float mine = logit_of(s, label, a.classes);
+    __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): they are read
+    if (row + (int)gridDim.x < a.rows) H::template fetch<AHEAD>(s + gridDim.x * a.ld, a.classes, g.tid, room);
+    logprob_row(a, g, h, s, row, label, mine);
+  }
+}
+
+// Rows divided among work-groups: group `part` of `parts` takes every chunk of CAPACITY elements from part * per_part on
+template <class T, int J>
+__global__ __launch_bounds__(256) void k_logprob_part(LogprobForward a, int parts, long per_part, PartRecord* records, Key* lists) {
+  typedef Held<T, 256, J> H;
+  __shared__ GroupSpace<256> space;
+  const Group<256> g{space, (int)threadIdx.x};
+  const unsigned unit = blockIdx.x;
+  const int row = (int)(unit / (unsigned)parts), part = (int)(unit - (unsigned)row * parts);
+  const T* s = (const T*)a.logits + row * a.ld;
+  const int label = label_of(a.labels, row);
   const bool has = label >= 0 && label < a.classes;
   const long c_begin = part * per_part, c_end = c_begin + per_part < a.classes ? c_begin + per_part : a.classes;
   RowSum v = RowSum::none();
@@ -438,37 +589,29 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_logprob_forward(Logprob
     return step;
   };
   long step = load(c_begin);
-  if (has) mine = to_f32(s[label]);
+  mine = logit_of(s, label, a.classes);
   for (long c0 = c_begin;;) {
     float quarter[4];
     const float largest = h.largest(quarter);
     const RowSum w = sum_of(g, h, largest);
     if (c0 == c_begin) v = w; else v.merge(w);
-    if (has) before += count_before(h, (int)c0, label, mine, H::E);
+    if (has) before += count_before(h, (int)c0, label, mine);
     const bool more = c0 + step < c_end;
     if (a.top && !v.broken()) {
-      unsigned best[4] = {0, 0, 0, 0};
-      if (NT == 64) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) best[i] = quarter[i] > -INF ? order_of(quarter[i]) : 0;
-      } else if (largest > -INF) {
-        best[0] = order_of(largest);
-      }
+      unsigned best[4];
+      orders<256>(best, quarter, largest);
       if ((unsigned)(held >> 32) > best[0]) best[0] = (unsigned)(held >> 32);
-      const float lz = v.empty() ? 0.f : log1pf(v.rest);
-#pragma unroll
-      for (int j = 0; j < J; ++j) h.renew(j);
+      h.renew();
       g.select(a.top, best, [&](float border, auto f) {
         if (held && value_of(held) >= border) f(held);
-        h.each([&](float t, int j, int e) { if (t >= border) f(key_of(t, (int)c0 + h.first(j) + e)); }, false);
+        h.each([&](float t, int j, int e) { if (t >= border) f(key_of(t, (int)c0 + h.first(j) + e)); });
       }, [&](int i) -> Key {
         if (i < a.top) return i < kept ? g.sh.list[i] : 0;             // classes of earlier chunks come first
         const float t = to_f32(s[c0 + i - a.top]);
         return t > -INF ? key_of(t, (int)c0 + i - a.top) : 0;
       }, (int)step + a.top, [&](int j, Key k) {
         if (more) g.sh.next[j] = k;                                    // the list goes on, in LDS
-        else if (parts == 1) write_entry(a, row, j, k, v, lz);
-        else lists[unit * a.top + j] = k;
+        else lists[(long)unit * a.top + j] = k;
       });
       if (more) {
         held = g.tid < a.top ? g.sh.next[g.tid] : 0;
@@ -482,14 +625,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_logprob_forward(Logprob
     step = load(c0);
   }
   if (a.top && v.broken())
-    for (int j = g.tid; j < a.top; j += NT) {
-      if (parts == 1) write_entry(a, row, j, 0, v, 0.f);
-      else lists[unit * a.top + j] = 0;
-    }
+    for (int j = g.tid; j < a.top; j += 256) lists[(long)unit * a.top + j] = 0;
   before = g.total(before);
-  if (g.tid) return;
-  if (parts == 1) write_row(a, row, v, before, label, has, mine);
-  else records[unit] = PartRecord{v, before};
+  if (g.tid == 0) records[unit] = PartRecord{v, before};
 }
 
 // a.parts <= 256 records and lists of a row
@@ -520,58 +658,47 @@ __global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int part
 }
 
 // ---- gradient of log probability and entropy ---------------------------------------------------------------------------
-// 16-byte units of all rows, one after the other; where logits and dlogits do not share their place within a unit, element by element
+// Every work-group has 1024 16-byte units of a row, all on their way before the first is used
 template <class T>
 __global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a, unsigned blocks_per_row) {
-  constexpr int E = 16 / sizeof(T), U = 4;
+  constexpr int U = 4;
+  typedef Held<T, 256, U> H;
   const int row = (int)(blockIdx.x / blocks_per_row);
   const int b = (int)(blockIdx.x - (unsigned)row * blocks_per_row);
   const T* s = (const T*)a.logits + row * a.ld;
   T* d = (T*)a.dlogits + row * a.ldd;
+  // blocks of whole units, counted from the 16-byte boundary at or before the row
+  const int shift = (int)(((uintptr_t)s & 15) / sizeof(T));
+  const long c0 = b ? (long)b * H::CAPACITY - shift : 0, c1 = (long)(b + 1) * H::CAPACITY - shift;
+  if (c0 >= a.classes) return;
+  H h;
+  h.load(s + c0, (int)((c1 < a.classes ? c1 : a.classes) - c0), threadIdx.x);
   const int label = a.grad_logprob ? a.labels[row] : -1;
   const float m = a.stats[2 * (long)row], lz = a.stats[2 * (long)row + 1];
   float g = label != -1 ? a.grad_logprob[row] : 0.f;
   if (label < -1 || label >= a.classes) g = quiet_nan();
-  const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.f, h = a.grad_entropy ? a.entropy[row] : 0.f;
+  const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.f, entropy = a.grad_entropy ? a.entropy[row] : 0.f;
   const float ng = -g, ngh = -gh;
   auto grad = [&](float x) {
     const float logp = (x - m) - lz, p = __builtin_amdgcn_exp2f(logp * LOG2E);
     // p is 0 below exp(-104), in a masked class for one, and the entropy's p log p with it
-    return m == -INF ? 0.f : p * fmaf(ngh, fmaxf(logp, -120.f) + h, ng);
+    return m == -INF ? 0.f : p * fmaf(ngh, fmaxf(logp, -120.f) + entropy, ng);
   };
   auto grad_label = [&](float x) {             // 1 - p from log p
     const float logp = (x - m) - lz, p = __builtin_amdgcn_exp2f(logp * LOG2E);
-    return m == -INF ? 0.f : fmaf(ngh * p, fmaxf(logp, -120.f) + h, ng * expm1f(logp));
+    return m == -INF ? 0.f : fmaf(ngh * p, fmaxf(logp, -120.f) + entropy, ng * expm1f(logp));
   };
-  const int shift = (int)(((uintptr_t)s & 15) / sizeof(T));
-  const bool alike = (((uintptr_t)s ^ (uintptr_t)d) & 15) == 0;
+  const int at_label = label - (int)c0;
+  h.store(d + c0, [&](float x, int j, int e) { return grad(x); });
+  // the label's, once more
+  const int unit = (at_label + h.shift) / H::E;
+  if (label >= 0 && label < a.classes && at_label >= 0 && at_label < h.len && unit % 256 == h.tid) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const long e0 = ((long)b * (256 * U) + u * 256 + threadIdx.x) * E - shift;
-    if (e0 >= a.classes) break;
-    if (alike && e0 >= 0 && e0 + E <= a.classes) {
-      float x[E], y[E];
-      if constexpr (sizeof(T) == 2) {
-        load8((const bf16_t*)s + e0, x);
-      } else {
-        const float4 q = *reinterpret_cast<const float4*>((const float*)s + e0);
-        x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
-      }
+    for (int j = 0; j < U; ++j)
+      if (unit / 256 == j)
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = grad(x[e]);
-      if (label >= e0 && label < e0 + E)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (e0 + e == label) y[e] = grad_label(x[e]);
-      if constexpr (sizeof(T) == 2) store8((bf16_t*)d + e0, y);
-      else *reinterpret_cast<float4*>((float*)d + e0) = make_float4(y[0], y[1], y[2], y[3]);
-    } else {
-      for (int e = 0; e < E; ++e)
-        if (e0 + e >= 0 && e0 + e < a.classes) {
-          const float x = to_f32(s[e0 + e]);
-          from_f32(d + e0 + e, e0 + e == label ? grad_label(x) : grad(x));
-        }
-    }
+        for (int e = 0; e < H::E; ++e)
+          if (h.first(j) + e == at_label) from_f32(d + label, grad_label(h.get(j, e)));
   }
 }
 
@@ -652,6 +779,7 @@ template <int HARD, class T, int NT, int J>
 __device__ __forceinline__ Soft soft_of(const Group<NT>& g, Held<T, NT, J>& h, float it) {
   float quarter[4];
   const float largest = h.largest(quarter), m = g.max(largest), mm = m == -INF ? 0.f : m, ct = LOG2E * it;
+  h.renew();
   float v[3] = {0.f, 0.f, 0.f};                // rest at T, rest at 1, classes at the maximum
   if (NT == 64 || __any(largest == m)) {
     h.each([&](float s, int, int) {
@@ -686,10 +814,10 @@ struct Answer {
 
   // what does not need the row's sums: loads that are on their way with the row
   __device__ __forceinline__ Answer(const Distill& a_, const T* s_, int row_) : a(a_), s(s_), row(row_) {
-    label = a.labels ? a.labels[row] : -1;
+    label = label_of(a.labels, row);
     has = label >= 0 && label < a.classes;
     weight = a.row_weight ? a.row_weight[row] : 1.f;
-    mine = has ? to_f32(s[label]) : 0.f;
+    mine = logit_of(s, label, a.classes);
   }
   __device__ __forceinline__ void finish(const Soft& v_, bool some, bool list_broken) {
     v = v_;
@@ -710,72 +838,47 @@ struct Answer {
     if (has && hw != 0.0) loss -= hw * logl;
     a.loss[row] = bad ? quiet_nan() : empty ? 0.f : (float)loss;
   }
-  // the gradient at the listed classes and the label, where q - p and p - 1 may cancel, among classes [c0, c1); by one wave
-  __device__ __forceinline__ void write_entries(const List& l, T* d, long c0, long c1, int lane) const {
-    if (bad || empty) return;
+  // The gradient at the listed classes and the label, where q - p and p - 1 may cancel: by one wave, before the others are written
+  struct Entries { int index, label; float at_index, at_label; };      // -1: none
+  __device__ __forceinline__ Entries entries(const List& l, int lane) const {
+    Entries r{-1, -1, 0.f, 0.f};
+    if (bad || empty) return r;
     const bool listed = __any(l.on && l.index == label);
-    if (l.on && l.index >= c0 && l.index < c1) {
+    if (l.on) {
       const double hard = wh == 0.0 ? 0.0 : l.index == label ? expm1(logl) : (double)expf(l.mine - v.m) / (1.0 + (double)v.rest1);
-      from_f32(d + l.index, (float)(ws * l.diff + wh * hard));
+      r.index = l.index;
+      r.at_index = (float)(ws * l.diff + wh * hard);
     }
-    if (has && !listed && label >= c0 && label < c1 && lane == 0) {
+    if (has && !listed && lane == 0) {
       const double q = (double)expf((mine - v.m) * (1.f / a.temperature)) / (1.0 + (double)v.restt);
-      from_f32(d + label, (float)(ws * q + wh * expm1(logl)));
+      r.label = label;
+      r.at_label = (float)(ws * q + wh * expm1(logl));
     }
+    return r;
+  }
+  static __device__ __forceinline__ void write(const Entries& r, T* d, long c0, long c1) {       // those among classes [c0, c1)
+    if (r.index >= c0 && r.index < c1) from_f32(d + r.index, r.at_index);
+    if (r.label >= c0 && r.label < c1) from_f32(d + r.label, r.at_label);
   }
 };
 
 // gradient of the `len` held elements to d
 template <int HARD, class T, int NT, int J>
 __device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero) {
-  typedef Held<T, NT, J> H;
   const float ct = LOG2E * it;
-  const bool alike = (int)(((uintptr_t)d & 15) / sizeof(T)) == h.shift;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    if (!h.used(j)) break;
-    h.renew(j);
-    float x[H::E];
-#pragma unroll
-    for (int e = 0; e < H::E; ++e) {
-      const float t = h.get(j, e) - m, et = __builtin_amdgcn_exp2f(t * ct);
-      x[e] = fs * et;
-      if (HARD) x[e] = fmaf(fh, hard_exp<HARD>(t, et), x[e]);
-      if (zero) x[e] = 0.f;
-    }
-    const int e0 = h.first(j);
-    if (alike && h.inside(j)) {
-      if (sizeof(T) == 2) {
-        uint4 q;
-        q.x = pack_bf16x2(x[0], x[1]); q.y = pack_bf16x2(x[2], x[3]);
-        q.z = pack_bf16x2(x[H::E - 4], x[H::E - 3]); q.w = pack_bf16x2(x[H::E - 2], x[H::E - 1]);
-        *reinterpret_cast<uint4*>(d + e0) = q;
-      } else {
-        *reinterpret_cast<float4*>(d + e0) = make_float4(x[0], x[1], x[2], x[3]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < H::E; ++e)
-        if (e0 + e >= 0 && e0 + e < h.len) from_f32(d + e0 + e, x[e]);
-    }
-  }
+  h.renew();
+  h.store(d, [&](float s, int, int) {
+    const float t = s - m, et = __builtin_amdgcn_exp2f(t * ct);
+    float x = fs * et;
+    if (HARD) x = fmaf(fh, hard_exp<HARD>(t, et), x);
+    return zero ? 0.f : x;
+  });
 }
 
-// a row that a group holds whole
+// A row that a group holds whole
 template <int HARD, class T, int NT, int J>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill(Distill a) {
-  constexpr int PER = NT < 256 ? 256 / NT : 1;
-  __shared__ GroupSpace<NT> space[PER];
-  const Group<NT> g{space[threadIdx.x / NT], (int)threadIdx.x % NT};
-  const int row = blockIdx.x * PER + threadIdx.x / NT;
-  if (row >= a.rows) return;
-  const T* s = (const T*)a.logits + row * a.ld;
+__device__ __forceinline__ void distill_row(const Distill& a, const Group<NT>& g, Held<T, NT, J>& h, Answer<T>& ans, List& l, int row) {
   const float it = 1.f / a.temperature;
-  Held<T, NT, J> h;
-  h.load(s, a.classes, g.tid);
-  Answer<T> ans(a, s, row);
-  List l{};
-  if (g.tid < 64) l = read_list(a, s, row, g.tid);
   const Soft v = soft_of<HARD>(g, h, it);
   // every wave needs to know whether the list has entries and bad ones; the first one has read it
   bool some = l.some, broken = l.broken;
@@ -790,9 +893,80 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill(Distill a) {
   if (g.tid == 0) ans.write_loss(l);
   if (!a.dlogits) return;
   T* d = (T*)a.dlogits + row * a.ldd;
+  typename Answer<T>::Entries entries{-1, -1, 0.f, 0.f};
+  if (g.tid < 64) entries = ans.entries(l, g.tid);
   write_gradient<HARD>(h, d, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad);
   if (NT > 64) __syncthreads(); else __builtin_amdgcn_s_waitcnt(0x0f70);   // the stores above are done before the entries replace some of them
-  if (g.tid < 64) ans.write_entries(l, d, 0, a.classes, g.tid);
+  if (g.tid < 64) Answer<T>::write(entries, d, 0, a.classes);
+}
+template <int HARD, class T, int NT, int J>
+__global__ __launch_bounds__(256) void k_distill(Distill a) {
+  constexpr int PER = 256 / NT;
+  __shared__ GroupSpace<NT> space[PER];
+  const int which = NT == 256 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
+  const Group<NT> g{space[which], (int)threadIdx.x % NT};
+  const int row = blockIdx.x * PER + which;
+  if (row >= a.rows) return;
+  const T* s = (const T*)a.logits + row * a.ld;
+  Held<T, NT, J> h;
+  h.load(s, a.classes, g.tid);
+  Answer<T> ans(a, s, row);
+  List l{};
+  if (g.tid < 64) l = read_list(a, s, row, g.tid);
+  distill_row<HARD>(a, g, h, ans, l, row);
+}
+// Long rows, like k_logprob_rows.  Loss and entries are left to k_distill_entries, which finds the rows' sums in `records`: their double
+// arithmetic next to a row in registers costs more registers than there are.
+template <int HARD, class T, int J, int AHEAD>
+__global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records) {
+  typedef Held<T, 1024, J> H;
+  __shared__ GroupSpace<1024> space;
+  extern __shared__ __align__(16) uint4 room[];
+  const Group<1024> g{space, (int)threadIdx.x};
+  const float it = 1.f / a.temperature;
+  int row = blockIdx.x;
+  const T* s = (const T*)a.logits + row * a.ld;
+  H::template fetch<AHEAD>(s, a.classes, g.tid, room);
+  for (; row < a.rows; row += gridDim.x) {
+    s = (const T*)a.logits + row * a.ld;
+    H h;
+    __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the thread's units are in LDS
+    h.template load<AHEAD>(s, a.classes, g.tid, room);
+    const int label = label_of(a.labels, row);
+    const bool has = label >= 0 && label < a.classes;
+    const float w = a.row_weight ? a.row_weight[row] : 1.f;
+    if (g.tid < 64) {
+      const int index = g.tid < a.top ? a.top_index[(long)row * a.top + g.tid] : -1;
+      const bool on = index >= 0 && a.top_logit[(long)row * a.top + g.tid] != -INF;
+      const bool some = __any(on), broken = __any(on && index >= a.classes);
+      if (g.tid == 0) space.n = (int)some | (int)broken << 1;
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): they are read
+    if (row + (int)gridDim.x < a.rows) H::template fetch<AHEAD>(s + gridDim.x * a.ld, a.classes, g.tid, room);
+    const Soft v = soft_of<HARD>(g, h, it);
+    const bool some = space.n & 1, empty = v.m == -INF;
+    const bool bad = v.m == INF || v.restt != v.restt || (HARD && v.rest1 != v.rest1) || (space.n & 2) || (label != -1 && !has);
+    if (g.tid == 0) records[row] = v;
+    if (a.dlogits) {
+      const float fs = bad ? quiet_nan() : some ? w * (1.f - a.hard_weight) * a.temperature / (1.f + v.restt) : 0.f;
+      const float fh = bad ? quiet_nan() : HARD && has ? w * a.hard_weight / (1.f + v.rest1) : 0.f;
+      write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, fs, fh, empty && !bad);
+    }
+    __syncthreads();                                   // space.n is read
+  }
+}
+template <class T>
+__global__ __launch_bounds__(256) void k_distill_entries(Distill a, const Soft* __restrict__ records) {
+  const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64)), lane = threadIdx.x & 63;
+  if (row >= a.rows) return;
+  const T* s = (const T*)a.logits + row * a.ld;
+  Answer<T> ans(a, s, row);
+  List l = read_list(a, s, row, lane);
+  const Soft v = records[row];
+  finish_list(a, l, v);
+  ans.finish(v, l.some, l.broken);
+  if (lane == 0) ans.write_loss(l);
+  if (a.dlogits) Answer<T>::write(ans.entries(l, lane), (T*)a.dlogits + row * a.ldd, 0, a.classes);
 }
 
 // a row divided among work-groups: first their sums ...
@@ -846,7 +1020,7 @@ __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long
     write_gradient<HARD>(h, d + c0, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad);
   }
   __syncthreads();
-  if (tid < 64) ans.write_entries(l, d, c_begin, c_end, tid);
+  if (tid < 64) Answer<T>::write(ans.entries(l, tid), d, c_begin, c_end);
 }
 
 // ---- how rows are cut ------------------------------------------------------------------------------------------------
@@ -882,6 +1056,16 @@ RowCut row_cut(int dt, int rows, int classes, bool aligned) {
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 bool aligned16(const void* p, long ld, size_t elem) { return ((uintptr_t)p & 15) == 0 && ((size_t)ld * elem & 15) == 0; }
 
+// one work-group of 1024 threads per CU with `ahead` units per thread in LDS
+template <class K, class A, class... MORE>
+hipError_t launch_rows(K kernel, int ahead, hipStream_t s, const A& a, MORE... more) {
+  const int lds = 1024 * 16 * ahead;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)(a.rows < CUS ? a.rows : CUS), 1024, lds, s>>>(a, more...);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hipStream_t s) {
   const RowCut c = row_cut(dt, a.rows, a.classes, aligned16(a.logits, a.ld, sizeof(T)));
@@ -889,14 +1073,14 @@ hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hip
     const unsigned n = (unsigned)((long)a.rows * c.parts);
     PartRecord* records = (PartRecord*)workspace;
     Key* lists = (Key*)((char*)workspace + align256((size_t)n * sizeof(PartRecord)));
-    k_logprob_forward<T, 256, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records, lists);
+    k_logprob_part<T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records, lists);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     k_logprob_join<T><<<(unsigned)a.rows, 256, 0, s>>>(a, c.parts, records, lists);
-  } else if (c.units <= 64 * 4) k_logprob_forward<T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
-  else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
-  else if (c.units <= 512 * 16) k_logprob_forward<T, 512, 16><<<(unsigned)a.rows, 512, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
-  else k_logprob_forward<T, 1024, 16><<<(unsigned)a.rows, 1024, 0, s>>>(a, 1, a.classes, nullptr, nullptr);
+  } else if (c.units <= 64 * 4) k_logprob_forward<T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
+  else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
+  else if (c.units <= 1024 * 8) return launch_rows(k_logprob_rows<T, 8, 8>, 8, s, a);
+  else return launch_rows(k_logprob_rows<T, 16, 8>, 8, s, a);
   return hipGetLastError();
 }
 
@@ -920,9 +1104,13 @@ hipError_t distill_as(int dt, const Distill& a, void* workspace, hipStream_t s) 
     if (e != hipSuccess) return e;
     k_distill_join<ANY, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
   } else if (c.units <= 64 * 4) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
-  else if (c.units <= 256 * 8) k_distill<HARD, T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
-  else if (c.units <= 512 * 16) k_distill<HARD, T, 512, 16><<<(unsigned)a.rows, 512, 0, s>>>(a);
-  else k_distill<HARD, T, 1024, 16><<<(unsigned)a.rows, 1024, 0, s>>>(a);
+  else if (c.units <= 256 * 8) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
+  else {
+    Soft* records = (Soft*)workspace;
+    const hipError_t e = c.units <= 1024 * 8 ? launch_rows(k_distill_rows<HARD, T, 8, 8>, 8, s, a, records) : launch_rows(k_distill_rows<HARD, T, 16, 8>, 8, s, a, records);
+    if (e != hipSuccess) return e;
+    k_distill_entries<T><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a, records);
+  }
   return hipGetLastError();
 }
 
@@ -940,7 +1128,8 @@ hipError_t distill(int dt, const Distill& a, void* workspace, hipStream_t s) {
 size_t logits_workspace_bytes(int dt, int rows, int classes, int top) {
   const RowCut c = row_cut(dt, rows, classes, false);
   const size_t n = (size_t)rows * c.parts;
-  return c.parts > 1 ? align256(n * sizeof(PartRecord)) + align256(n * top * sizeof(Key)) : 0;
+  if (c.parts > 1) return align256(n * sizeof(PartRecord)) + align256(n * top * sizeof(Key));
+  return c.units > 256 * 8 ? align256(n * sizeof(Soft)) : 0;
 }
 
 hipError_t launch_logprob_forward(int dt, const LogprobForward& a, void* workspace, hipStream_t stream) {

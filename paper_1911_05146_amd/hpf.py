@@ -499,6 +499,12 @@ class Ops:
             raise ValueError(f"{name}: strides {t.stride()}: columns must be contiguous and rows must not overlap")
         return t.data_ptr(), ld
 
+    def _like_rows(self, t, ld):
+        """An empty matrix with t's shape and row stride: where the logits' rows start on 16 bytes their gradient's do too."""
+        rows, cols = t.shape
+        return self.torch.empty((rows, ld), dtype=self.tdtype, device=self.device)[:, :cols] if ld != cols else \
+            self.torch.empty((rows, cols), dtype=self.tdtype, device=self.device)
+
     def _dense(self, name, t, shape, dtype):
         if t is None:
             return 0
@@ -610,7 +616,7 @@ class Ops:
         lp, ld = self._rows("logits", logits)
         rows, classes = logits.shape
         f32 = torch.float32
-        d = out if out is not None else torch.empty((rows, classes), dtype=self.tdtype, device=self.device)
+        d = out if out is not None else self._like_rows(logits, ld)
         dp, ldd = self._rows("out", d, (rows, classes))
         with torch.cuda.device(self.device):
             hpf_op_logprob_backward(self.dt, lp, ld, self._labels(labels, rows), self._dense("stats", stats, (rows, 2), f32),
@@ -628,13 +634,13 @@ class Ops:
         ti = self._dense("top_index", top_index, (rows, top), torch.int32)
         tl = self._dense("top_logit", top_logit, (rows, top), torch.float32)
         loss = torch.empty(rows, dtype=torch.float32, device=self.device)
-        d = torch.empty((rows, classes), dtype=self.tdtype, device=self.device) if gradient else None
+        d = self._like_rows(logits, ld) if gradient else None
         with torch.cuda.device(self.device):
             n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
             ws, wsp = self._scratch(n)
             hpf_op_distill(self.dt, lp, ld, ti, tl, top, self._labels(labels, rows), temperature, hard_weight,
                            self._dense("row_weight", row_weight, (rows,), torch.float32), loss.data_ptr(),
-                           d.data_ptr() if gradient else 0, classes, rows, classes, wsp, n, self._s())
+                           d.data_ptr() if gradient else 0, ld, rows, classes, wsp, n, self._s())
         return loss, d
 
 
