@@ -388,72 +388,83 @@ struct Held {
       for (int e = 0; e < E; ++e) f(get(j, e), j, e);
     }
   }
-  // largest of the thread's elements; part[]: of the units j with j % 4 == i
-  __device__ __forceinline__ float largest(float (&part)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) part[i] = -INF;
-    each([&](float s, int j, int) { part[j & 3] = fmaxf(part[j & 3], s); });
-    return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-  }
 };
 
-// How many classes are before `label`, whose logit is `mine`: larger ones, and equal ones of lower index.  base: class of p's first element.
-// Counted per wave, one comparison per element: units before the label's take the next smaller number as their border.
-template <class H>
-__device__ __forceinline__ int count_before(H& h, int base, int label, float mine) {
-  constexpr int E = H::E;
-  int n = 0;
-  h.renew();
-  if (mine == -INF) {                          // a masked label, for which there is no smaller number
-    h.each([&](float s, int j, int e) {
-      const int c = h.first(j) + e;
-      n += __popcll(__ballot(s > mine || (s == mine && c >= 0 && c < h.len && base + c < label)));
-    });
-    return n;
-  }
-  const unsigned b = __float_as_uint(mine);
-  const float below = mine == 0.f ? -__uint_as_float(1) : __uint_as_float(mine > 0.f ? b - 1 : b + 1);
-  float border = 0.f;
-  h.each([&](float s, int j, int e) {
-    if (e == 0) border = base + h.first(j) + E <= label ? below : mine;
-    n += __popcll(__ballot(s > border));
-  });
-  // the label's own unit: equal logits in front of it, counted by the thread that holds it
-  const int at = label - base + h.shift;       // counted from the first unit's start
-  if (label < base || label - base >= h.len) return n;
-  const int unit = at / E, uj = unit / H::THREADS, ut = unit % H::THREADS;
-#pragma unroll
-  for (int j = 0; j < H::UNITS; ++j)
-    if (uj == j)
-#pragma unroll
-      for (int e = 0; e < E; ++e) n += __popcll(__ballot(h.tid == ut && e < at % E && h.get(j, e) == mine));
-  return n;
+// v_max3_f32: fmaxf would spend an instruction more per operand on signalling NaNs
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 
-// {m, rest, dot} of what a group holds.  Only waves that hold a maximum keep it apart from the sum.
+// One pass: the largest of the thread's elements, part[]: of the units j with j % 4 == i; and how many classes are before `label`, whose logit is
+// `mine`: larger ones, and equal ones of lower index (COUNT; per wave).  base: class of the first element.  Counted with one comparison per
+// element: units before the label's take the next smaller number as their border.
+template <bool COUNT, class H>
+__device__ __forceinline__ float look(H& h, float (&part)[4], int base, int label, float mine, int& before) {
+  constexpr int E = H::E;
+  const unsigned b = __float_as_uint(mine);
+  const float below = mine == 0.f ? -__uint_as_float(1) : __uint_as_float(mine > 0.f ? b - 1 : b + 1);
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[i] = -INF;
+#pragma unroll
+  for (int j = 0; j < H::UNITS; ++j) {
+    if (!h.used(j)) break;
+    const float border = base + h.first(j) + E <= label ? below : mine;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float x = h.get(j, e), y = h.get(j, e + 1);
+      part[j & 3] = max3(part[j & 3], x, y);
+      if (COUNT) n += __popcll(__ballot(x > border)) + __popcll(__ballot(y > border));
+    }
+  }
+  if (COUNT) {
+    if (mine == -INF) {                        // a masked label, for which there is no smaller number
+      n = 0;
+      h.each([&](float s, int j, int e) {
+        const int c = h.first(j) + e;
+        n += __popcll(__ballot(s > mine || (s == mine && c >= 0 && c < h.len && base + c < label)));
+      });
+    } else if (label >= base && label - base < h.len) {
+      // the label's own unit: equal logits in front of it, counted by the thread that holds it
+      const int at = label - base + h.shift, unit = at / E, uj = unit / H::THREADS, ut = unit % H::THREADS;
+#pragma unroll
+      for (int j = 0; j < H::UNITS; ++j)
+        if (uj == j)
+#pragma unroll
+          for (int e = 0; e < E; ++e) n += __popcll(__ballot(h.tid == ut && e < at % E && h.get(j, e) == mine));
+    }
+    before = n;
+  }
+  return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+
+// {m, rest, dot} of what a group holds.  Only waves that hold a maximum keep it apart from the sum.  (s - m) log2 e stays a subtraction and a
+// product: as one multiply-add it would be off by the rounding of m log2 e, without bound for large m.
 template <class T, int NT, int J>
 __device__ __forceinline__ RowSum sum_of(const Group<NT>& g, Held<T, NT, J>& h, float largest) {
   const float m = g.max(largest), mm = m == -INF ? 0.f : m;
   h.renew();
-  float v[3] = {0.f, 0.f, 0.f};                // rest, dot, classes at the maximum
+  float v[3] = {0.f, 0.f, 0.f};                // rest, dot (times log2 e), classes at the maximum
   if (NT == 64 || __any(largest == m)) {
     int ties = 0;
     h.each([&](float s, int, int) {
-      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * LOG2E);
-      v[0] += d == 0.f ? 0.f : e;
-      v[1] = fmaf(e, fmaxf(d, -3e38f), v[1]);
-      ties += __popcll(__ballot(d == 0.f));
+      const float x = (s - mm) * LOG2E, e = __builtin_amdgcn_exp2f(x);
+      v[0] += x == 0.f ? 0.f : e;
+      v[1] = fmaf(e, fmaxf(x, -200.f), v[1]);
+      ties += __popcll(__ballot(x == 0.f));
     });
     v[2] = (g.tid & 63) == 0 ? (float)ties : 0.f;
   } else {
     h.each([&](float s, int, int) {
-      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * LOG2E);
+      const float x = (s - mm) * LOG2E, e = __builtin_amdgcn_exp2f(x);     // 0 below -150, in a masked class for one
       v[0] += e;
-      v[1] = fmaf(e, fmaxf(d, -3e38f), v[1]);
+      v[1] = fmaf(e, fmaxf(x, -200.f), v[1]);
     });
   }
   g.reduce(v, [](float a, float b) { return a + b; });
-  return RowSum{m, m == -INF ? v[0] : v[0] + (v[2] - 1.f), v[1]};
+  return RowSum{m, m == -INF ? v[0] : v[0] + (v[2] - 1.f), v[1] * 0.693147181f};
 }
 
 // ---- log probabilities ------------------------------------------------------------------------------------------------
@@ -492,15 +503,30 @@ __device__ __forceinline__ void orders(unsigned (&best)[4], const float (&quarte
   }
 }
 
+// f for the keys of all elements >= border
+template <class H, class F>
+__device__ __forceinline__ void above(const H& h, const float (&quarter)[4], float border, int base, F f) {
+#pragma unroll
+  for (int j = 0; j < H::UNITS; ++j) {
+    if (!h.used(j)) break;
+    if (quarter[j & 3] >= border)
+#pragma unroll
+      for (int e = 0; e < H::E; ++e) {
+        const float t = h.get(j, e);
+        if (t >= border) f(key_of(t, base + h.first(j) + e));
+      }
+  }
+}
+
 // A row that a group holds whole.  s, label and mine are the same in all lanes.
 template <class T, int NT, int J>
 __device__ __forceinline__ void logprob_row(const LogprobForward& a, const Group<NT>& g, Held<T, NT, J>& h, const T* s, int row, int label, float mine) {
   const bool has = label >= 0 && label < a.classes;
   float quarter[4];
-  const float largest = h.largest(quarter);
-  const RowSum v = sum_of(g, h, largest);
   int before = 0;
-  if (has) before = g.total(count_before(h, 0, label, mine));
+  const float largest = has ? look<true>(h, quarter, 0, label, mine, before) : look<false>(h, quarter, 0, label, mine, before);
+  const RowSum v = sum_of(g, h, largest);
+  if (has) before = g.total(before);
   if (g.tid == 0) write_row(a, row, v, before, label, has, mine);
   if (!a.top) return;
   if (v.broken()) {
@@ -511,9 +537,7 @@ __device__ __forceinline__ void logprob_row(const LogprobForward& a, const Group
   orders<NT>(best, quarter, largest);
   const float lz = v.empty() ? 0.f : log1pf(v.rest);
   h.renew();
-  g.select(a.top, best, [&](float border, auto f) {
-    h.each([&](float t, int j, int e) { if (t >= border) f(key_of(t, h.first(j) + e)); });
-  }, [&](int i) -> Key {
+  g.select(a.top, best, [&](float border, auto f) { above(h, quarter, border, 0, f); }, [&](int i) -> Key {
     const float t = to_f32(s[i]);
     return t > -INF ? key_of(t, i) : 0;
   }, a.classes, [&](int j, Key k) { write_entry(a, row, j, k, v, lz); });
@@ -592,10 +616,11 @@ __global__ __launch_bounds__(256) void k_logprob_part(LogprobForward a, int part
   mine = logit_of(s, label, a.classes);
   for (long c0 = c_begin;;) {
     float quarter[4];
-    const float largest = h.largest(quarter);
+    int n = 0;
+    const float largest = has ? look<true>(h, quarter, (int)c0, label, mine, n) : look<false>(h, quarter, (int)c0, label, mine, n);
+    before += n;
     const RowSum w = sum_of(g, h, largest);
     if (c0 == c_begin) v = w; else v.merge(w);
-    if (has) before += count_before(h, (int)c0, label, mine);
     const bool more = c0 + step < c_end;
     if (a.top && !v.broken()) {
       unsigned best[4];
@@ -604,7 +629,7 @@ __global__ __launch_bounds__(256) void k_logprob_part(LogprobForward a, int part
       h.renew();
       g.select(a.top, best, [&](float border, auto f) {
         if (held && value_of(held) >= border) f(held);
-        h.each([&](float t, int j, int e) { if (t >= border) f(key_of(t, (int)c0 + h.first(j) + e)); });
+        above(h, quarter, border, (int)c0, f);
       }, [&](int i) -> Key {
         if (i < a.top) return i < kept ? g.sh.list[i] : 0;             // classes of earlier chunks come first
         const float t = to_f32(s[c0 + i - a.top]);
@@ -766,33 +791,43 @@ __device__ __forceinline__ void finish_list(const Distill& a, List& l, const Sof
 // exp at temperature 1 next to exp at temperature T: HARD_EXP of its own, or HARD_ONE / HARD_TWO / HARD_FOUR: e^(1/T) to the power T = 1, 2, 4
 // (an exponential costs four times a multiplication)
 enum : int { HARD_NONE = 0, HARD_EXP = 1, HARD_ONE = 2, HARD_TWO = 3, HARD_FOUR = 4 };
-template <int HARD>
-__device__ __forceinline__ float hard_exp(float d, float et) {
-  if (HARD == HARD_ONE) return et;
-  if (HARD == HARD_TWO) return et * et;
-  if (HARD == HARD_FOUR) { const float q = et * et; return q * q; }
-  return __builtin_amdgcn_exp2f(d * LOG2E);
-}
+struct Exponents {
+  float m, ct;
+  __device__ __forceinline__ Exponents(float m_, float it) : m(m_ == -INF ? 0.f : m_), ct(it * LOG2E) {}
+  __device__ __forceinline__ float soft(float s) const { return __builtin_amdgcn_exp2f((s - m) * ct); }
+  template <int HARD>
+  __device__ __forceinline__ float hard(float s, float et) const {
+    if (HARD == HARD_ONE) return et;
+    if (HARD == HARD_TWO) return et * et;
+    if (HARD == HARD_FOUR) { const float q = et * et; return q * q; }
+    return __builtin_amdgcn_exp2f((s - m) * LOG2E);
+  }
+};
 
-// Sums of what a group holds at temperatures 1 (if HARD) and T
+// Sums of what a group holds at temperatures 1 (if HARD) and T, as in sum_of
 template <int HARD, class T, int NT, int J>
 __device__ __forceinline__ Soft soft_of(const Group<NT>& g, Held<T, NT, J>& h, float it) {
   float quarter[4];
-  const float largest = h.largest(quarter), m = g.max(largest), mm = m == -INF ? 0.f : m, ct = LOG2E * it;
+  int none;
+  const float largest = look<false>(h, quarter, 0, -1, 0.f, none), m = g.max(largest);
+  const Exponents x(m, it);
   h.renew();
   float v[3] = {0.f, 0.f, 0.f};                // rest at T, rest at 1, classes at the maximum
   if (NT == 64 || __any(largest == m)) {
+    int ties = 0;
     h.each([&](float s, int, int) {
-      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * ct);
-      v[0] += d == 0.f ? 0.f : e;
-      if (HARD) v[1] += d == 0.f ? 0.f : hard_exp<HARD>(d, e);
-      v[2] += d == 0.f ? 1.f : 0.f;
+      const bool is = s == m;
+      const float e = x.soft(s);
+      v[0] += is ? 0.f : e;
+      if (HARD) v[1] += is ? 0.f : x.hard<HARD>(s, e);
+      ties += __popcll(__ballot(is));
     });
+    v[2] = (g.tid & 63) == 0 ? (float)ties : 0.f;
   } else {
     h.each([&](float s, int, int) {
-      const float d = s - mm, e = __builtin_amdgcn_exp2f(d * ct);
+      const float e = x.soft(s);
       v[0] += e;
-      if (HARD) v[1] += hard_exp<HARD>(d, e);
+      if (HARD) v[1] += x.hard<HARD>(s, e);
     });
   }
   g.reduce(v, [](float a, float b) { return a + b; });
@@ -865,13 +900,13 @@ struct Answer {
 // gradient of the `len` held elements to d
 template <int HARD, class T, int NT, int J>
 __device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero) {
-  const float ct = LOG2E * it;
+  const Exponents x(m, it);
   h.renew();
   h.store(d, [&](float s, int, int) {
-    const float t = s - m, et = __builtin_amdgcn_exp2f(t * ct);
-    float x = fs * et;
-    if (HARD) x = fmaf(fh, hard_exp<HARD>(t, et), x);
-    return zero ? 0.f : x;
+    const float e = x.soft(s);
+    float y = fs * e;
+    if (HARD) y = fmaf(fh, x.hard<HARD>(s, e), y);
+    return zero ? 0.f : y;
   });
 }
 
