@@ -252,12 +252,15 @@ __device__ __forceinline__ void tile_of(unsigned i, unsigned rows, unsigned cols
 
 // BM x BN tile by WM x WN waves; 64 of the contraction per step, two stages in LDS, loaded past the registers.  A stage's row is 128 bytes;
 // its 16-byte units are stored in the order unit ^ (row & 7), so that 8 neighbouring rows' reads of one unit fall on all banks.
+// A step has two halves of 32.  While the matrix cores work on the first, the fragments of the second are read; in the middle of the second comes
+// the step's only barrier, behind which the next stage is complete (its loads were issued a whole step ago) and this one free for the loads of
+// the step after, and the first fragments of the next step are read under the remaining products.
 template <int BM, int BN, int WM, int WN, int OUT>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigned tile_rows, unsigned tile_cols, int steps_per_split) {
   constexpr int NT = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * 64;
   constexpr int LA = BM * 8 / NT, LB = BN * 8 / NT;      // 16-byte units per thread and step
   extern __shared__ __align__(16) bf16_t smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   unsigned tr, tc;
   tile_of(blockIdx.x, tile_rows, tile_cols, tr, tc);
@@ -265,32 +268,41 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   const int k_begin = (int)blockIdx.y * steps_per_split, k_all = (p.K + 63) / 64;
   const int steps = (k_all - k_begin < steps_per_split ? k_all - k_begin : steps_per_split);
 
-  // thread: rows tid / 8 + i * NT / 8, unit tid % 8 of the stage, which holds unit (tid ^ row) % 8 of the operand
+  // thread: rows tid / 8 + i * NT / 8, unit tid % 8 of the stage, which holds unit (tid ^ row) % 8 of the operand.  Rows behind the last one read
+  // the last one; offsets within a tile fit 32 bits (256 rows of 2^20).
   const int unit = (tid ^ (tid >> 3)) & 7;
-  const bf16_t* pa[LA];
-  const bf16_t* pb[LB];
+  uint32_t oa[LA], ob[LB];
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
-    const int r = m0 + (tid >> 3) + i * (NT / 8);
-    pa[i] = p.A + (r < p.M ? r : p.M - 1) * p.lda + k_begin * 64 + unit * 8;
+    const int r = (tid >> 3) + i * (NT / 8), last = p.M - 1 - m0;
+    oa[i] = (uint32_t)((r < last ? r : last) * p.lda + unit * 8) * 2u;
   }
 #pragma unroll
   for (int i = 0; i < LB; ++i) {
-    const int r = n0 + (tid >> 3) + i * (NT / 8);
-    pb[i] = p.B + (r < p.N ? r : p.N - 1) * p.ldb + k_begin * 64 + unit * 8;
+    const int r = (tid >> 3) + i * (NT / 8), last = p.N - 1 - n0;
+    ob[i] = (uint32_t)((r < last ? r : last) * p.ldb + unit * 8) * 2u;
   }
-  const int k_left = p.K - k_begin * 64 - unit * 8;      // > 0: the unit of step 0 is there
-  auto load = [&](int step, int st) {
-    bf16_t* s = smem + st * STAGE + wave * 512;
+  const char* ga = (const char*)(p.A + m0 * p.lda + k_begin * 64);
+  const char* gb = (const char*)(p.B + n0 * p.ldb + k_begin * 64);
+  const int k_left = p.K - k_begin * 64;
+  auto load = [&](int step) {
+    bf16_t* s = smem + (step & 1) * STAGE + wave * 512;
+    const char* a = ga + step * 128;
+    const char* b = gb + step * 128;
+    if (k_left >= (step + 1) * 64) {
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-      const bf16_t* g = k_left > step * 64 ? pa[i] + step * 64 : (const bf16_t*)kZeros;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, (__attribute__((address_space(3))) void*)(s + i * (NT * 8)), 16, 0, 0);
+      for (int i = 0; i < LA; ++i)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a + oa[i]), (__attribute__((address_space(3))) void*)(s + i * (NT * 8)), 16, 0, 0);
+    } else {                                             // the contraction ends within this step
+      const bool there = k_left > step * 64 + unit * 8;
+#pragma unroll
+      for (int i = 0; i < LA; ++i)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(there ? a + oa[i] : (const char*)kZeros),
+                                         (__attribute__((address_space(3))) void*)(s + i * (NT * 8)), 16, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pb[i] + step * 64),
-                                       (__attribute__((address_space(3))) void*)(s + BM * 64 + i * (NT * 8)), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(b + ob[i]), (__attribute__((address_space(3))) void*)(s + BM * 64 + i * (NT * 8)), 16, 0, 0);
   };
 
   floatx4 acc[TN][TM];
@@ -302,26 +314,45 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   const int row = lane & 15, q = lane >> 4;
   const int at_a = (wm * (BM / WM) + row) * 64, at_b = BM * 64 + (wn * (BN / WN) + row) * 64;
   const int u0 = ((q) ^ (row & 7)) * 8, u1 = ((q + 4) ^ (row & 7)) * 8;
-  load(0, 0);
-  for (int t = 0; t < steps; ++t) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): this step's units are in LDS
-    __syncthreads();
-    if (t + 1 < steps) load(t + 1, (t + 1) & 1);
-    const bf16_t* s = smem + (t & 1) * STAGE;
+  struct Frags { bf16x8 a[TM], b[TN]; };
+  auto read = [&](Frags& f, int step, int u) {
+    const bf16_t* s = smem + (step & 1) * STAGE;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int u = h ? u1 : u0;
-      bf16x8 a[TM], b[TN];
+    for (int i = 0; i < TN; ++i) f.b[i] = *reinterpret_cast<const bf16x8*>(s + at_b + i * 1024 + u);
 #pragma unroll
-      for (int i = 0; i < TN; ++i) b[i] = *reinterpret_cast<const bf16x8*>(s + at_b + i * 1024 + u);
+    for (int j = 0; j < TM; ++j) f.a[j] = *reinterpret_cast<const bf16x8*>(s + at_a + j * 1024 + u);
+  };
+  auto multiply = [&](const Frags& f, int j0, int j1) {
 #pragma unroll
-      for (int j = 0; j < TM; ++j) a[j] = *reinterpret_cast<const bf16x8*>(s + at_a + j * 1024 + u);
+    for (int j = j0; j < j1; ++j)
 #pragma unroll
-      for (int j = 0; j < TM; ++j)
-#pragma unroll
-        for (int i = 0; i < TN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[i], a[j], acc[i][j], 0, 0, 0);
-    }
+      for (int i = 0; i < TN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b[i], f.a[j], acc[i][j], 0, 0, 0);
+  };
+  Frags f0, f1;
+  load(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+  __syncthreads();
+  if (steps > 1) load(1);
+  read(f0, 0, u0);
+  for (int t = 0; t + 1 < steps; ++t) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);                  // lgkmcnt(0): f0, which was asked for half of a half ago
+    read(f1, t, u1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f0, 0, TM);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f1, 0, TM / 2);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): this thread's units of the next stage are in LDS
+    __builtin_amdgcn_s_barrier();                        // everybody's are, and everybody has this stage's fragments
+    read(f0, t + 1, u0);
+    if (t + 2 < steps) load(t + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f1, TM / 2, TM);
+    __builtin_amdgcn_sched_barrier(0);
   }
+  read(f1, steps - 1, u1);
+  multiply(f0, 0, TM);
+  multiply(f1, 0, TM);
   __syncthreads();
 
   // A wave's results go through its own part of LDS, 16 rows at a time, so that a lane ends up with 8 consecutive columns
