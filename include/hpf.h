@@ -412,7 +412,7 @@ hpf_status hpf_op_bn_relu_forward_noalloc(hpf_dtype dtype, const void* x, const 
  * (w [K][N]).  HPF_BF16: the products take bf16 copies of the weights, which hpf_op_linear_pack lays out once after every
  * change of w (2 * (N * ceil64(K) + K * ceil64(N)) bytes, 256-byte aligned), and sum in fp32.  HPF_F32 (check mode): `weights`
  * is w itself, products and sums are in double.
- *   M <= 2^21, K, N <= 2^20 (else HPF_EUNSUPPORTED). */
+ *   M <= 2^21, K, N <= 2^20, no matrix of more than 2^32 elements (else HPF_EUNSUPPORTED). */
 typedef enum { HPF_ACT_NONE = 0, HPF_ACT_RELU = 1, HPF_ACT_GELU = 2 /* z * Phi(z) */, HPF_ACT_SILU = 3 /* z / (1 + exp(-z)) */ } hpf_activation;
 size_t hpf_op_linear_packed_bytes(int32_t K, int32_t N);
 hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed, size_t packed_bytes, void* hip_stream);

@@ -42,93 +42,97 @@ __device__ __forceinline__ void activate(int act, A z, A& y, A& slope) {
 }
 
 // An operand of the contraction: element (row, k) at p[row * rs + k * ks]
-template <class T>
-struct Operand { const T* p; long rs, ks; };
-template <class T>
+struct Operand { const float* p; long rs, ks; };
 struct Epilogue {
   const float* bias;
-  const T* residual; long ldr;
-  T* y; long ldy;
-  T* slope;
+  const float* residual; long ldr;
+  float* y; long ldy;
+  float* slope;
   float* sum; int accumulate;     // instead of y: C in fp32, [M][N]
   int act;
 };
 
-template <class T> struct Mma;
-template <> struct Mma<bf16_t> {
-  typedef float Acc;
-  typedef floatx4 Acc4;
-  static constexpr int K = 32;
-  typedef bf16x8 Frag;
-  static __device__ __forceinline__ Frag frag(const bf16_t* row, int lane) { return *reinterpret_cast<const bf16x8*>(row + (lane >> 4) * 8); }
-  static __device__ __forceinline__ Acc4 mma(Frag a, Frag b, Acc4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ int row(int lane, int r) { return (lane >> 4) * 4 + r; }   // of the first operand; column lane & 15
-};
-template <> struct Mma<float> {
-  typedef double Acc;
-  typedef doublex4 Acc4;
-  static constexpr int K = 4;
-  typedef double Frag;
-  static __device__ __forceinline__ Frag frag(const float* row, int lane) { return (double)row[lane >> 4]; }
-  static __device__ __forceinline__ Acc4 mma(Frag a, Frag b, Acc4 c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ int row(int lane, int r) { return (lane >> 4) + 4 * r; }
-};
-
-// C tile of 64 x 64 by four waves, 32 x 32 each; 32 steps of the contraction staged in LDS at a time.  Any sizes and strides.
-template <class T>
-__global__ __launch_bounds__(256) void k_linear_tile(Operand<T> A, Operand<T> B, Epilogue<T> e, int M, int N, int K) {
-  typedef Mma<T> X;
-  constexpr int KS = 32, LS = KS + 8;
-  __shared__ __align__(16) T sA[64 * LS], sB[64 * LS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
-  typename X::Acc4 acc[2][2] = {};
-  auto stage = [&](const Operand<T>& o, T* s, int r0, int rows, int k0) {
-    for (int i = tid; i < 64 * KS; i += 256) {
-      const int r = o.ks == 1 ? i / KS : i % 64, k = o.ks == 1 ? i % KS : i / 64;
-      s[r * LS + k] = r0 + r < rows && k0 + k < K ? o.p[(long)(r0 + r) * o.rs + (long)(k0 + k) * o.ks] : T(0);
+// fp32 (check mode): C tile of 32 x 32 by eight waves, four of 16 x 16 for each half of the 64 steps that are staged at a time; the halves are
+// joined at the end.  v_mfma_f64_16x16x4_f64 takes 64 cycles, so small tiles, which give every CU one, cost nothing: 333 x 1000 x 517 has 187 of
+// them (64 x 64 ones with four waves: 54, and 144 us instead of TILE_F32 us).  Any sizes and strides.
+__global__ __launch_bounds__(512) void k_linear_tile_f32(Operand A, Operand B, Epilogue e, int M, int N, int K) {
+  constexpr int KS = 64, LS = KS + 4;
+  __shared__ __align__(16) float sA[32 * LS], sB[32 * LS];
+  __shared__ double join[4][64][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = wave >> 2;
+  const unsigned cols = (unsigned)(N + 31) / 32;
+  const int m0 = (int)(blockIdx.x / cols) * 32, n0 = (int)(blockIdx.x % cols) * 32;
+  const int wm = (wave & 1) * 16, wn = (wave >> 1 & 1) * 16;
+  doublex4 acc = {0.0, 0.0, 0.0, 0.0};
+  float ra[4], rb[4];
+  // a thread's four elements of an operand's 32 x 64: along whichever of row and k is contiguous
+  auto at = [&](const Operand& o, int i, int& r, int& k) {
+    if (o.ks == 1) { r = tid >> 4; k = (tid & 15) * 4 + i; }
+    else { r = tid & 31; k = (tid >> 5) + 16 * i; }
+  };
+  auto load = [&](const Operand& o, int r0, int rows, int k0, float (&v)[4]) {
+    int r, k;
+    at(o, 0, r, k);
+    if (o.ks == 1 && r0 + r < rows && k0 + k + 4 <= K) {
+      const float* p = o.p + (long)(r0 + r) * o.rs + k0 + k;
+      if (((uintptr_t)p & 15) == 0) {
+        const float4 q = *reinterpret_cast<const float4*>(p);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      at(o, i, r, k);
+      v[i] = r0 + r < rows && k0 + k < K ? o.p[(long)(r0 + r) * o.rs + (long)(k0 + k) * o.ks] : 0.f;
     }
   };
+  auto put = [&](const Operand& o, float* s, const float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int r, k;
+      at(o, i, r, k);
+      s[r * LS + k] = v[i];
+    }
+  };
+  load(A, m0, M, 0, ra);
+  load(B, n0, N, 0, rb);
   for (int k0 = 0; k0 < K; k0 += KS) {
     __syncthreads();
-    stage(A, sA, m0, M, k0);
-    stage(B, sB, n0, N, k0);
+    put(A, sA, ra);
+    put(B, sB, rb);
     __syncthreads();
+    if (k0 + KS < K) {
+      load(A, m0, M, k0 + KS, ra);
+      load(B, n0, N, k0 + KS, rb);
+    }
 #pragma unroll
-    for (int k = 0; k < KS; k += X::K) {
-      typename X::Frag a[2], b[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        a[i] = X::frag(&sA[(wm + i * 16 + (lane & 15)) * LS + k], lane);
-        b[i] = X::frag(&sB[(wn + i * 16 + (lane & 15)) * LS + k], lane);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = X::mma(b[j], a[i], acc[i][j]);   // rows: n, columns: m
+    for (int k = 0; k < KS / 2; k += 4) {
+      const int c = part * (KS / 2) + k + (lane >> 4);
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)sB[(wn + (lane & 15)) * LS + c], (double)sA[(wm + (lane & 15)) * LS + c], acc, 0, 0, 0);
     }
   }
+  if (part)
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int r = 0; r < 4; ++r) join[wave & 3][lane][r] = acc[r];
+  __syncthreads();
+  if (part) return;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int m = m0 + wm + i * 16 + (lane & 15), n = n0 + wn + j * 16 + X::row(lane, r);
-        if (m >= M || n >= N) continue;
-        typename X::Acc z = acc[i][j][r], y, slope;
-        if (e.sum) {
-          float* o = e.sum + (long)m * N + n;
-          *o = (float)(e.accumulate ? z + *o : z);
-          continue;
-        }
-        if (e.bias) z += e.bias[n];
-        activate(e.act, z, y, slope);
-        if (e.residual) y += to_f32(e.residual[m * e.ldr + n]);
-        from_f32(e.y + m * e.ldy + n, (float)y);
-        if (e.slope) from_f32(e.slope + (long)m * N + n, (float)slope);
-      }
+  for (int r = 0; r < 4; ++r) {
+    const int m = m0 + wm + (lane & 15), n = n0 + wn + (lane >> 4) + 4 * r;      // rows of the first operand: n
+    if (m >= M || n >= N) continue;
+    double z = acc[r] + join[wave][lane][r], y, slope;
+    if (e.sum) {
+      float* o = e.sum + (long)m * N + n;
+      *o = (float)(e.accumulate ? z + *o : z);
+      continue;
+    }
+    if (e.bias) z += e.bias[n];
+    activate(e.act, z, y, slope);
+    if (e.residual) y += e.residual[m * e.ldr + n];
+    e.y[m * e.ldy + n] = (float)y;
+    if (e.slope) e.slope[(long)m * N + n] = (float)slope;
+  }
 }
 
 // ---- bf16: tiles on matrix cores -------------------------------------------------------------------------------------
@@ -145,7 +149,7 @@ struct Product {
   bf16_t* y; long ldy;
   bf16_t* slope;
   int act;
-  // OUT_SUM: C in fp32 [M][N]; OUT_SLAB: this share's C, [splits][M][N]
+  // OUT_SUM: C in fp32 [M][N]; OUT_SLAB: this share's C, [splits][M][slab_row(N)]
   float* sum; int accumulate;
 };
 
@@ -174,6 +178,8 @@ __device__ __forceinline__ void activate_fast(int act, float z, float& y, float&
   }
 }
 
+__host__ __device__ constexpr int slab_row(int n) { return (n + 7) & ~7; }       // rows of partial sums start on 32 bytes
+
 // Eight consecutive results of a row, n a multiple of 8.  The bias and, where rows allow 16-byte loads, the residual are asked for ahead of the
 // sums they join: one at a time they cost a trip to memory for every 16 rows of a tile (residual, bias, gelu and slope at 8192 x 4096 x 4096:
 // 65 us on top of the product, now 43).
@@ -194,9 +200,13 @@ __device__ __forceinline__ uint4 residual8(const Product& p, int m, int n) {
 template <int OUT>
 __device__ __forceinline__ void finish8(const Product& p, int m, int n, float (&v)[8], unsigned split, const Ahead& a, const uint4& res) {
   const int left = p.N - n;
-  if (OUT != OUT_Y) {
-    float* o = p.sum + ((size_t)(OUT == OUT_SLAB ? split : 0) * p.M + m) * p.N + n;
-    const bool add = OUT == OUT_SUM && p.accumulate;
+  if (OUT == OUT_SLAB) {
+    store8(p.sum + ((size_t)split * p.M + m) * slab_row(p.N) + n, v);
+    return;
+  }
+  if (OUT == OUT_SUM) {
+    float* o = p.sum + (size_t)m * p.N + n;
+    const bool add = p.accumulate;
     if (left >= 8 && (p.N & 3) == 0) {
       if (add) {
         float w[8];
@@ -267,12 +277,22 @@ __device__ __forceinline__ void tile_of(unsigned i, unsigned rows, unsigned cols
   r = r0 + (u - c * h);
 }
 
-// BM x BN tile by WM x WN waves; 64 of the contraction per step, two stages in LDS, loaded past the registers.  A stage's row is 128 bytes;
+// s_waitcnt vmcnt(n), and lgkmcnt(0) with it
+constexpr int wait_loads(int n) { return 0x0070 | (n & 15) | (n >> 4) << 14; }
+
+// A barrier that no access to LDS is moved across; what has to be waited for, the caller waits for
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// BM x BN tile by WM x WN waves; 64 of the contraction per step, STAGES of them in LDS, loaded past the registers.  A stage's row is 128 bytes;
 // its 16-byte units are stored in the order unit ^ (row & 7), so that 8 neighbouring rows' reads of one unit fall on all banks.
 // A step has two halves of 32.  While the matrix cores work on the first, the fragments of the second are read; between them comes the step's only
-// barrier, behind which the next stage is complete (its loads were issued a whole step ago) and this one free for the loads of the step
-// after, and the first fragments of the next step are read under the products of the second half.
-template <int BM, int BN, int WM, int WN, int OUT>
+// barrier, behind which the next stage is complete (its loads were issued STAGES - 1 steps ago) and this one free for the loads of a later
+// step, and the first fragments of the next step are read under the products of the second half.
+template <int BM, int BN, int WM, int WN, int STAGES, int OUT>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigned tile_rows, unsigned tile_cols, int steps_per_split) {
   constexpr int NT = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * 64;
   constexpr int LA = BM * 8 / NT, LB = BN * 8 / NT;      // 16-byte units per thread and step
@@ -303,7 +323,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   const char* gb = (const char*)(p.B + n0 * p.ldb + k_begin * 64);
   const int k_left = p.K - k_begin * 64;
   auto load = [&](int step) {
-    bf16_t* s = smem + (step & 1) * STAGE + wave * 512;
+    bf16_t* s = smem + (step % STAGES) * STAGE + wave * 512;
     const char* a = ga + step * 128;
     const char* b = gb + step * 128;
     if (k_left >= (step + 1) * 64) {
@@ -333,7 +353,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   const int u0 = ((q) ^ (row & 7)) * 8, u1 = ((q + 4) ^ (row & 7)) * 8;
   struct Frags { bf16x8 a[TM], b[TN]; };
   auto read = [&](Frags& f, int step, int u) {
-    const bf16_t* s = smem + (step & 1) * STAGE;
+    const bf16_t* s = smem + (step % STAGES) * STAGE;
 #pragma unroll
     for (int i = 0; i < TN; ++i) f.b[i] = *reinterpret_cast<const bf16x8*>(s + at_b + i * 1024 + u);
 #pragma unroll
@@ -346,10 +366,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
       for (int i = 0; i < TN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b[i], f.a[j], acc[i][j], 0, 0, 0);
   };
   Frags f0, f1;
-  load(0);
-  __builtin_amdgcn_s_waitcnt(0x0f70);
-  __syncthreads();
-  if (steps > 1) load(1);
+#pragma unroll
+  for (int t = 0; t < STAGES; ++t)
+    if (t < steps) load(t);
+  if (steps >= STAGES) __builtin_amdgcn_s_waitcnt(wait_loads((STAGES - 1) * (LA + LB)));
+  else __builtin_amdgcn_s_waitcnt(wait_loads(0));
+  stage_barrier();
   read(f0, 0, u0);
   for (int t = 0; t + 1 < steps; ++t) {
     __builtin_amdgcn_s_waitcnt(0xc07f);                  // lgkmcnt(0): f0, which was asked for half of a half ago
@@ -357,10 +379,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
     __builtin_amdgcn_sched_barrier(0);
     multiply(f0, 0, TM);
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt(0): this thread's units of the next stage are in LDS
-    __builtin_amdgcn_s_barrier();                        // everybody's are, and everybody has this stage's fragments
+    // this thread's units of the next stage are in LDS, and f1 is here
+    if (t + STAGES <= steps) __builtin_amdgcn_s_waitcnt(wait_loads((STAGES - 2) * (LA + LB)));
+    else __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    stage_barrier();                                     // everybody's are, and everybody has this stage's fragments
     read(f0, t + 1, u0);
-    if (t + 2 < steps) load(t + 2);
+    if (t + STAGES < steps) load(t + STAGES);
     __builtin_amdgcn_sched_barrier(0);
     multiply(f1, 0, TM);
     __builtin_amdgcn_sched_barrier(0);
@@ -373,7 +397,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   // A wave's results go through its own part of LDS, 16 rows at a time, so that a lane ends up with 8 consecutive columns
   constexpr int TS = BN / WN + 4;                        // fp32 row stride: rows shift by 4 banks
   constexpr int LANES = BN / WN / 8, ROWS = 64 / LANES;  // lanes per row, rows per pass
-  static_assert(16 * TS * 4 * WM * WN <= 2 * STAGE * 2, "the rows of all waves fit the stages");
+  static_assert(16 * TS * 4 * WM * WN <= STAGES * STAGE * 2, "the rows of all waves fit the stages");
   float* mine = reinterpret_cast<float*>(smem) + wave * 16 * TS;
   const int n = n0 + wn * (BN / WN) + (lane % LANES) * 8, m_lane = m0 + wm * (BM / WM) + lane / LANES;
   const Ahead a = ahead<OUT>(p, n);
@@ -399,32 +423,72 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   }
 }
 
+// Up to 16 rows: the product is a reading of the weights.  A wave has 16 columns and an eighth of the work-group's share of the contraction, its
+// fragments straight from memory, 256 contiguous bytes of a weight row per round; the eight sums are joined in LDS.
+template <int OUT>
+__global__ __launch_bounds__(512) void k_linear_few(Product p, int steps_per_split) {
+  __shared__ __align__(16) float part[8][16][20];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, q = lane >> 4;
+  const int n0 = blockIdx.x * 16, k_all = (p.K + 31) / 32;
+  const int k_begin = (int)blockIdx.y * steps_per_split, k_end = k_begin + steps_per_split < k_all ? k_begin + steps_per_split : k_all;
+  const int share = ((k_end - k_begin + 7) / 8 + 3) & ~3, k0 = k_begin + wave * share, k1 = k0 + share < k_end ? k0 + share : k_end;
+  const bf16_t* a = p.A + (row < p.M ? row : p.M - 1) * p.lda + q * 8;
+  const bf16_t* b = p.B + (n0 + row < p.N ? n0 + row : p.N - 1) * p.ldb + q * 8;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  auto fragment = [&](const bf16_t* r, int k, bool there) { return *reinterpret_cast<const bf16x8*>(there ? r + k * 32 : (const bf16_t*)kZeros); };
+  for (int k = k0; k < k1; k += 8) {
+    bf16x8 fa[8], fb[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      fb[i] = fragment(b, k + i, k + i < k1);
+      fa[i] = fragment(a, k + i, k + i < k1 && (k + i) * 32 + q * 8 < p.K);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[i], fa[i], acc, 0, 0, 0);
+  }
+  *reinterpret_cast<floatx4*>(&part[wave][row][q * 4]) = acc;        // row: m, columns: n
+  __syncthreads();
+  if (tid >= 32) return;
+  const int m = tid >> 1, n = n0 + (tid & 1) * 8;
+  if (m >= p.M || n >= p.N) return;
+  float v[8] = {};
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    float t[8];
+    load8(&part[w][m][(tid & 1) * 8], t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += t[e];
+  }
+  finish8<OUT>(p, m, n, v, blockIdx.y, ahead<OUT>(p, n), residual8<OUT>(p, m, n));
+}
+
 // y or the sum from the shares of a split contraction
 template <int OUT>
 __global__ __launch_bounds__(256) void k_linear_join(Product p, const float* __restrict__ slabs, int splits) {
   const int units = (p.N + 7) / 8;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)p.M * units; i += (size_t)gridDim.x * 256) {
-    const int m = (int)(i / units), n = (int)(i - (size_t)m * units) * 8, left = p.N - n;
+    const int m = (int)(i / units), n = (int)(i - (size_t)m * units) * 8;
     const Ahead a = ahead<OUT>(p, n);
     const uint4 res = residual8<OUT>(p, m, n);
-    const float* o = slabs + (size_t)m * p.N + n;
-    const size_t slab = (size_t)p.M * p.N;
+    const float* o = slabs + (size_t)m * slab_row(p.N) + n;
+    const size_t slab = (size_t)p.M * slab_row(p.N);
     float v[8] = {};
     int s = 0;
-    if (left >= 8 && (p.N & 3) == 0) {
-      for (; s + 4 <= splits; s += 4) {                  // four shares on their way together
-        float w[4][8];
+    for (; s + 4 <= splits; s += 4) {                    // four shares on their way together
+      float w[4][8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load8(o + (s + k) * slab, w[k]);
+      for (int k = 0; k < 4; ++k) load8(o + (s + k) * slab, w[k]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += w[k][e];
-      }
+        for (int e = 0; e < 8; ++e) v[e] += w[k][e];
     }
-    for (; s < splits; ++s)
+    for (; s < splits; ++s) {
+      float w[8];
+      load8(o + s * slab, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += e < left ? o[s * slab + e] : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
     finish8<OUT>(p, m, n, v, 0, a, res);
   }
 }
@@ -584,26 +648,28 @@ __global__ __launch_bounds__(256) void k_linear_pack(const float* __restrict__ w
   }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void k_linear_dz(const T* __restrict__ dy, long lddy, const T* __restrict__ slope, T* __restrict__ dz, int M, int N) {
+// fp32: dz, and its column sums, 64 per work-group
+__global__ __launch_bounds__(256) void k_linear_dz_f32(const float* __restrict__ dy, long lddy, const float* __restrict__ slope, float* __restrict__ dz, int M, int N) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)M * N; i += (size_t)gridDim.x * 256) {
     const size_t m = i / N, n = i - m * N;
-    from_f32(dz + i, to_f32(dy[m * lddy + n]) * to_f32(slope[i]));
+    dz[i] = dy[m * lddy + n] * slope[i];
   }
 }
 
-// db: 64 columns per work-group
-template <class T>
-__global__ __launch_bounds__(256) void k_linear_db(const T* __restrict__ dz, long ld, float* __restrict__ db, int accumulate, int M, int N) {
-  __shared__ double part[4][64];
+__global__ __launch_bounds__(1024) void k_linear_db_f32(const float* __restrict__ dz, long ld, float* __restrict__ db, int accumulate, int M, int N) {
+  __shared__ double part[16][64];
   const int c = threadIdx.x & 63, g = threadIdx.x >> 6, n = blockIdx.x * 64 + c;
   double s = 0.0;
-  if (n < N)
-    for (int m = g; m < M; m += 4) s += to_f32(dz[m * ld + n]);
+  if (n < N) {
+    int m = g;
+    for (; m + 48 < M; m += 64) s += ((double)dz[m * ld + n] + dz[(m + 16) * ld + n]) + ((double)dz[(m + 32) * ld + n] + dz[(m + 48) * ld + n]);
+    for (; m < M; m += 16) s += dz[m * ld + n];
+  }
   part[g][c] = s;
   __syncthreads();
   if (g == 0 && n < N) {
-    s = part[0][c] + part[1][c] + part[2][c] + part[3][c];
+    s = 0.0;
+    for (int k = 0; k < 16; ++k) s += part[k][c];
     db[n] = (float)(accumulate ? s + db[n] : s);
   }
 }
@@ -615,22 +681,23 @@ unsigned grid_for(size_t n, size_t per, size_t cap) {
 }
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-// How a bf16 product is cut
+// How a bf16 product is cut: 256 x 256 tiles where they fill the chip, 128 x 128 ones where those do; else 128 x 64 ones with four stages on their
+// way, and the contraction split until there is a work-group per CU; up to 16 rows by k_linear_few.
+enum : int { CUT_LARGE, CUT_TILES, CUT_SPLIT, CUT_FEW };
 struct Cut {
-  bool large;
-  int splits, steps;            // steps of 64 per share
+  int kind, splits, steps;      // steps (of 64, CUT_FEW: 32) per share
   unsigned rows, cols;          // tiles
 };
 Cut cut_of(int M, int N, int K) {
+  auto tiles = [&](int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   Cut c;
-  const long big = (long)((M + 255) / 256) * ((N + 255) / 256);
-  c.large = big >= 192;
-  const int T = c.large ? 256 : 128;
-  c.rows = (unsigned)((M + T - 1) / T);
-  c.cols = (unsigned)((N + T - 1) / T);
-  const int k = (K + 63) / 64;
-  long want = c.large ? 1 : 512 / ((long)c.rows * c.cols);
-  if (want > k / 4) want = k / 4;
+  c.kind = M <= 16 ? CUT_FEW : tiles(256, 256) >= 192 ? CUT_LARGE : tiles(128, 128) >= 256 ? CUT_TILES : CUT_SPLIT;
+  const int bm = c.kind == CUT_FEW ? 16 : c.kind == CUT_LARGE ? 256 : 128, bn = c.kind == CUT_FEW ? 16 : c.kind == CUT_SPLIT ? 64 : bm;
+  c.rows = (unsigned)((M + bm - 1) / bm);
+  c.cols = (unsigned)((N + bn - 1) / bn);
+  const int unit = c.kind == CUT_FEW ? 32 : 64, k = (K + unit - 1) / unit, least = c.kind == CUT_FEW ? 32 : 8;
+  long want = c.kind == CUT_SPLIT || c.kind == CUT_FEW ? 256 / ((long)c.rows * c.cols) : 1;
+  if (want > k / least) want = k / least;
   if (want < 1) want = 1;
   c.steps = (int)((k + want - 1) / want);
   c.splits = (k + c.steps - 1) / c.steps;
@@ -638,13 +705,13 @@ Cut cut_of(int M, int N, int K) {
 }
 size_t slab_bytes(int M, int N, int K) {
   const Cut c = cut_of(M, N, K);
-  return c.splits > 1 ? align256((size_t)c.splits * M * N * sizeof(float)) : 0;
+  return c.splits > 1 ? align256((size_t)c.splits * M * slab_row(N) * sizeof(float)) : 0;
 }
 
-template <int BM, int BN, int WM, int WN, int OUT>
+template <int BM, int BN, int WM, int WN, int STAGES, int OUT>
 hipError_t mfma(const Product& p, const Cut& c, hipStream_t s) {
-  constexpr int lds = 2 * (BM + BN) * 64 * 2;
-  const auto kernel = k_linear_mfma<BM, BN, WM, WN, OUT>;
+  constexpr int lds = STAGES * (BM + BN) * 64 * 2;
+  const auto kernel = k_linear_mfma<BM, BN, WM, WN, STAGES, OUT>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
@@ -652,16 +719,22 @@ hipError_t mfma(const Product& p, const Cut& c, hipStream_t s) {
   kernel<<<dim3(c.rows * c.cols, (unsigned)c.splits), 64 * WM * WN, lds, s>>>(p, c.rows, c.cols, c.steps);
   return hipGetLastError();
 }
+template <int OUT>
+hipError_t few(const Product& p, const Cut& c, hipStream_t s) {
+  k_linear_few<OUT><<<dim3(c.cols, (unsigned)c.splits), 512, 0, s>>>(p, c.steps);
+  return hipGetLastError();
+}
 
 // OUT: OUT_Y or OUT_SUM; slabs: room for slab_bytes
 template <int OUT>
 hipError_t product(const Product& p, float* slabs, hipStream_t s) {
   const Cut c = cut_of(p.M, p.N, p.K);
-  if (c.large) return mfma<256, 256, 2, 4, OUT>(p, c, s);
-  if (c.splits == 1) return mfma<128, 128, 2, 2, OUT>(p, c, s);
+  if (c.kind == CUT_LARGE) return mfma<256, 256, 2, 4, 2, OUT>(p, c, s);
+  if (c.kind == CUT_TILES) return mfma<128, 128, 2, 2, 2, OUT>(p, c, s);
+  if (c.splits == 1) return c.kind == CUT_FEW ? few<OUT>(p, c, s) : mfma<128, 64, 2, 2, 4, OUT>(p, c, s);
   Product q = p;
   q.sum = slabs;
-  const hipError_t e = mfma<128, 128, 2, 2, OUT_SLAB>(q, c, s);
+  const hipError_t e = c.kind == CUT_FEW ? few<OUT_SLAB>(q, c, s) : mfma<128, 64, 2, 2, 4, OUT_SLAB>(q, c, s);
   if (e != hipSuccess) return e;
   k_linear_join<OUT><<<grid_for((size_t)p.M * ((p.N + 7) / 8), 256, 2048), 256, 0, s>>>(p, slabs, c.splits);
   return hipGetLastError();
@@ -744,13 +817,13 @@ hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
 }
 
 // ---- fp32 (check mode) -----------------------------------------------------------------------------------------------
-hipError_t tile(const Operand<float>& A, const Operand<float>& B, const Epilogue<float>& e, int M, int N, int K, hipStream_t s) {
-  k_linear_tile<float><<<dim3(blocks64(N), blocks64(M)), 256, 0, s>>>(A, B, e, M, N, K);
+hipError_t tile(const Operand& A, const Operand& B, const Epilogue& e, int M, int N, int K, hipStream_t s) {
+  k_linear_tile_f32<<<(unsigned)((N + 31) / 32) * (unsigned)((M + 31) / 32), 512, 0, s>>>(A, B, e, M, N, K);
   return hipGetLastError();
 }
 
 hipError_t forward_f32(const LinearForward& a, hipStream_t s) {
-  const Epilogue<float> e{a.bias, (const float*)a.residual, a.ldr, (float*)a.y, a.ldy, (float*)a.slope, nullptr, 0, a.act};
+  const Epilogue e{a.bias, (const float*)a.residual, a.ldr, (float*)a.y, a.ldy, (float*)a.slope, nullptr, 0, a.act};
   return tile({(const float*)a.x, a.ldx, 1}, {(const float*)a.weights, 1, a.N}, e, a.M, a.N, a.K, s);
 }
 
@@ -759,22 +832,22 @@ hipError_t backward_f32(const LinearBackward& a, float* ws, hipStream_t s) {
   long ld = a.lddy;
   hipError_t err = hipSuccess;
   if (a.slope) {
-    k_linear_dz<<<grid_for((size_t)a.M * a.N, 2048, 4096), 256, 0, s>>>(dz, ld, (const float*)a.slope, ws, a.M, a.N);
+    k_linear_dz_f32<<<grid_for((size_t)a.M * a.N, 2048, 4096), 256, 0, s>>>(dz, ld, (const float*)a.slope, ws, a.M, a.N);
     dz = ws;
     ld = a.N;
     err = hipGetLastError();
   }
   if (err == hipSuccess && a.db) {
-    k_linear_db<<<blocks64(a.N), 256, 0, s>>>(dz, ld, a.db, a.accumulate, a.M, a.N);
+    k_linear_db_f32<<<blocks64(a.N), 1024, 0, s>>>(dz, ld, a.db, a.accumulate, a.M, a.N);
     err = hipGetLastError();
   }
   if (err == hipSuccess && a.dx) {
-    Epilogue<float> e{};
+    Epilogue e{};
     e.y = (float*)a.dx; e.ldy = a.lddx;
     err = tile({dz, ld, 1}, {(const float*)a.weights, a.N, 1}, e, a.M, a.K, a.N, s);
   }
   if (err == hipSuccess && a.dw) {
-    Epilogue<float> e{};
+    Epilogue e{};
     e.sum = a.dw; e.accumulate = a.accumulate;
     err = tile({(const float*)a.x, 1, a.ldx}, {dz, 1, ld}, e, a.K, a.N, a.M, s);
   }

@@ -28,6 +28,9 @@ hpf_status linear_shape(hpf_dtype dtype, int32_t M, int32_t K, int32_t N, int& d
   if (!type_of(dtype, dt)) return fail(HPF_EINVAL, "unknown dtype");
   if (M < 0 || K < 1 || N < 1) return fail(HPF_EINVAL, "M must not be negative, K and N must be positive (%d, %d, %d)", M, K, N);
   if (K > MAX_WIDTH || N > MAX_WIDTH || M > (1 << 21)) return fail(HPF_EUNSUPPORTED, "more than 2^21 rows or 2^20 columns (%d, %d, %d)", M, K, N);
+  const int64_t most = (int64_t)1 << 32;
+  if ((int64_t)M * N > most || (int64_t)M * K > most || (int64_t)K * N > most)
+    return fail(HPF_EUNSUPPORTED, "a matrix of more than 2^32 elements (%d, %d, %d)", M, K, N);
   return HPF_OK;
 }
 hpf_status workspace_ok(const void* workspace, size_t bytes, size_t need) {
@@ -43,7 +46,8 @@ hpf_status workspace_ok(const void* workspace, size_t bytes, size_t need) {
 extern "C" {
 
 size_t hpf_op_linear_packed_bytes(int32_t K, int32_t N) {
-  return K < 1 || N < 1 || K > MAX_WIDTH || N > MAX_WIDTH ? 0 : linear_packed_elems(K, N) * sizeof(bf16_t);
+  int dt;
+  return linear_shape(HPF_BF16, 0, K, N, dt) != HPF_OK ? 0 : linear_packed_elems(K, N) * sizeof(bf16_t);
 }
 
 hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed, size_t packed_bytes, void* hip_stream) {

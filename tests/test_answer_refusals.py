@@ -51,6 +51,8 @@ def test_linear_refusals(hpf):
         g(EINVAL, "positive", N=0)
         g(EUN, "2^20", K=(1 << 20) + 1)
         g(EUN, "2^21", M=(1 << 21) + 1)
+        g(EUN, "2^32", M=1 << 21, N=(1 << 11) + 1, **({"ldy": 1 << 12} if g is f else {"lddy": 1 << 12}))
+        g(EUN, "2^32", K=1 << 20, N=1 << 13, **({"ldy": 1 << 13} if g is f else {"lddy": 1 << 13}))
         g(EINVAL, "stride", ldx=15)
         g(EINVAL, "aligned", x=A + 1 if g is f else B + 1)
         g(EINVAL, "256-byte", w=(B if g is f else D) + 64)
