@@ -550,11 +550,10 @@ __device__ __forceinline__ float logit_of(const T* s, int label, int classes) {
 }
 
 // rows that a wave or 256 threads hold: many of them on a CU at a time
-template <class T, int NT, int J>
-__global__ __launch_bounds__(256) void k_logprob_forward(LogprobForward a) {
-  constexpr int PER = 256 / NT;                        // rows per work-group
+template <class T, int NT, int J, int PER>       // PER: rows per work-group
+__global__ __launch_bounds__(NT * PER) void k_logprob_forward(LogprobForward a) {
   __shared__ GroupSpace<NT> space[PER];
-  const int which = NT == 256 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
+  const int which = PER == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
   const Group<NT> g{space[which], (int)threadIdx.x % NT};
   const int row = blockIdx.x * PER + which;
   if (row >= a.rows) return;                           // a whole wave, or nobody
@@ -655,6 +654,26 @@ __global__ __launch_bounds__(256) void k_logprob_part(LogprobForward a, int part
   if (g.tid == 0) records[unit] = PartRecord{v, before};
 }
 
+// The sums of a row from those of its parts, one per thread (RowSum::none() where there is none): seen from the largest maximum, which the first
+// part that holds it keeps out of its sum
+__device__ __forceinline__ bool holds_maximum(const Group<256>& g, float m, float& top) {
+  const Key k = g.max((Key)order_of(m) << 32 | (0xffffffffu - (unsigned)g.tid));
+  top = value_of(k);
+  return (unsigned)k == 0xffffffffu - (unsigned)g.tid;
+}
+__device__ __forceinline__ RowSum join_parts(const Group<256>& g, const RowSum& p) {
+  float m;
+  const bool base = holds_maximum(g, p.m, m);
+  float v[2] = {p.rest, p.dot};
+  if (!base && p.m != -INF) {
+    const float d = p.m - m, e = expf(d), z = 1.f + p.rest;
+    v[0] = z * e;
+    v[1] = e > 0.f || e != e ? e * (p.dot + d * z) : 0.f;
+  }
+  g.reduce(v, [](float a, float b) { return a + b; });
+  return RowSum{m, v[0], v[1]};
+}
+
 // a.parts <= 256 records and lists of a row
 template <class T>
 __global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int parts, const PartRecord* __restrict__ records, const Key* __restrict__ lists) {
@@ -665,16 +684,14 @@ __global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int part
   const int label = a.labels ? a.labels[row] : -1;
   const bool has = label >= 0 && label < a.classes;
   const float mine = has ? to_f32(s[label]) : 0.f;
-  __shared__ PartRecord rec[256];
-  if (g.tid < parts) rec[g.tid] = records[(long)row * parts + g.tid];
+  PartRecord rec{RowSum::none(), 0};
+  if (g.tid < parts) rec = records[(long)row * parts + g.tid];
   const Key* list = lists + (long)row * parts * a.top;
   const int n = parts * a.top;
   unsigned best[4] = {0, 0, 0, 0};
   for (int i = g.tid; i < n; i += 256) best[0] = (unsigned)(list[i] >> 32) > best[0] ? (unsigned)(list[i] >> 32) : best[0];
-  __syncthreads();
-  RowSum v = RowSum::none();
-  int before = 0;
-  for (int i = 0; i < parts; ++i) { v.merge(rec[i].sum); before += rec[i].before; }
+  const RowSum v = join_parts(g, rec.sum);
+  const int before = g.total(wave_all(rec.before, [](int a, int b) { return a + b; }));
   if (g.tid == 0) write_row(a, row, v, before, label, has, mine);
   if (!a.top) return;
   const float lz = v.empty() ? 0.f : log1pf(v.rest);
@@ -934,11 +951,10 @@ __device__ __forceinline__ void distill_row(const Distill& a, const Group<NT>& g
   if (NT > 64) __syncthreads(); else __builtin_amdgcn_s_waitcnt(0x0f70);   // the stores above are done before the entries replace some of them
   if (g.tid < 64) Answer<T>::write(entries, d, 0, a.classes);
 }
-template <int HARD, class T, int NT, int J>
-__global__ __launch_bounds__(256) void k_distill(Distill a) {
-  constexpr int PER = 256 / NT;
+template <int HARD, class T, int NT, int J, int PER>
+__global__ __launch_bounds__(NT * PER) void k_distill(Distill a) {
   __shared__ GroupSpace<NT> space[PER];
-  const int which = NT == 256 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
+  const int which = PER == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
   const Group<NT> g{space[which], (int)threadIdx.x % NT};
   const int row = blockIdx.x * PER + which;
   if (row >= a.rows) return;
@@ -1030,14 +1046,22 @@ __global__ __launch_bounds__(256) void k_distill_part(Distill a, int parts, long
 template <int HARD, class T, int J>
 __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long per_part, const Soft* __restrict__ records) {
   typedef Held<T, 256, J> H;
-  __shared__ Soft rec[256];
+  __shared__ GroupSpace<256> space;
+  const Group<256> g{space, (int)threadIdx.x};
   const int row = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - (unsigned)row * parts), tid = threadIdx.x;
   const T* s = (const T*)a.logits + row * a.ld;
   const float it = 1.f / a.temperature;
-  if (tid < parts) rec[tid] = records[(long)row * parts + tid];
-  __syncthreads();
-  Soft v = rec[0];
-  for (int i = 1; i < parts; ++i) merge(v, rec[i], it);
+  Soft p{-INF, 0.f, 0.f};
+  if (tid < parts) p = records[(long)row * parts + tid];
+  Soft v;
+  float sum[2] = {p.rest1, p.restt};
+  if (!holds_maximum(g, p.m, v.m) && p.m != -INF) {
+    sum[0] = (1.f + p.rest1) * expf(p.m - v.m);
+    sum[1] = (1.f + p.restt) * expf((p.m - v.m) * it);       // at temperature T the distance of the maxima counts 1 / T of itself
+  }
+  g.reduce(sum, [](float a, float b) { return a + b; });
+  v.rest1 = sum[0];
+  v.restt = sum[1];
   List l = read_list(a, s, row, tid & 63);
   finish_list(a, l, v);
   Answer<T> ans(a, s, row);
@@ -1060,6 +1084,7 @@ __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long
 
 // ---- how rows are cut ------------------------------------------------------------------------------------------------
 constexpr int CUS = 256, MAX_PARTS = 256, PART_J = 4;
+constexpr int SPREAD_ROWS = 4 * CUS;     // up to so many short rows get a work-group each, on all CUs, instead of one of four
 
 struct RowCut {
   int parts;
@@ -1112,8 +1137,10 @@ hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hip
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     k_logprob_join<T><<<(unsigned)a.rows, 256, 0, s>>>(a, c.parts, records, lists);
-  } else if (c.units <= 64 * 4) k_logprob_forward<T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
-  else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
+  } else if (c.units <= 64 * 4) {
+    if (a.rows <= SPREAD_ROWS) k_logprob_forward<T, 64, 4, 1><<<(unsigned)a.rows, 64, 0, s>>>(a);
+    else k_logprob_forward<T, 64, 4, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
+  } else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8, 1><<<(unsigned)a.rows, 256, 0, s>>>(a);
   else if (c.units <= 1024 * 8) return launch_rows(k_logprob_rows<T, 8, 8>, 8, s, a);
   else return launch_rows(k_logprob_rows<T, 16, 8>, 8, s, a);
   return hipGetLastError();
@@ -1138,8 +1165,11 @@ hipError_t distill_as(int dt, const Distill& a, void* workspace, hipStream_t s) 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     k_distill_join<ANY, T, PART_J><<<n, 256, 0, s>>>(a, c.parts, c.per_part, records);
-  } else if (c.units <= 64 * 4) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 64, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
-  else if (c.units <= 256 * 8) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a);
+  } else if (c.units <= 64 * 4) {
+    constexpr int ANY = HARD ? HARD_EXP : HARD_NONE;
+    if (a.rows <= SPREAD_ROWS) k_distill<ANY, T, 64, 4, 1><<<(unsigned)a.rows, 64, 0, s>>>(a);
+    else k_distill<ANY, T, 64, 4, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
+  } else if (c.units <= 256 * 8) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 256, 8, 1><<<(unsigned)a.rows, 256, 0, s>>>(a);
   else {
     Soft* records = (Soft*)workspace;
     const hipError_t e = c.units <= 1024 * 8 ? launch_rows(k_distill_rows<HARD, T, 8, 8>, 8, s, a, records) : launch_rows(k_distill_rows<HARD, T, 16, 8>, 8, s, a, records);

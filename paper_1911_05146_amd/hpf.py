@@ -417,6 +417,7 @@ class Ops:
         self.tdtype = torch.bfloat16 if compute_dtype == HPF_BF16 else torch.float32
         self.device = torch.device(device)
         self._ws = None
+        self._index = self.device.index
 
     def workspace(self, cin, cout, R):
         n = hpf_op_workspace_bytes(cin, cout, R)
@@ -479,25 +480,39 @@ class Ops:
 
     # ---- the answer end of a model.  Tensors are of this object's type (rows may have a stride), on its device; work goes to
     # the device's current stream, workspaces come from torch's allocator of that stream.
+    def _enqueue(self, call, *args):
+        """call(*args, stream) on the device's current stream.  Small calls take the host longer than the GPU, so nothing is asked twice."""
+        cuda = self.torch.cuda
+        here = cuda.current_device()
+        index = here if self._index is None else self._index
+        if here == index:
+            call(*args, cuda.current_stream(index).cuda_stream)
+        else:
+            with cuda.device(index):
+                call(*args, cuda.current_stream(index).cuda_stream)
+
     def _here(self, t):
-        return t.device == self.device or (self.device.index is None and t.device.type == self.device.type
+        return t.device == self.device or (self._index is None and t.device.type == self.device.type
                                            and t.device.index == self.torch.cuda.current_device())
 
-    def _rows(self, name, t, shape=None, dtype=None):
+    def _rows(self, name, t, shape=None):
         """(address, row stride) of a matrix; raises ValueError for what the library could not tell from an address."""
         if t is None:
             return 0, 0
-        if t.dtype != (dtype or self.tdtype):
-            raise ValueError(f"{name}: expected {dtype or self.tdtype}, got {t.dtype}")
+        if t.dtype is not self.tdtype:
+            raise ValueError(f"{name}: expected {self.tdtype}, got {t.dtype}")
         if not self._here(t):
             raise ValueError(f"{name}: on {t.device}, expected {self.device}")
-        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape or '[rows, columns]'}")
-        rows, cols = t.shape
-        ld = t.stride(0) if rows > 1 else max(cols, 1)
-        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        got = t.shape
+        if len(got) != 2 or (shape is not None and got != shape):
+            raise ValueError(f"{name}: shape {tuple(got)}, expected {shape or '[rows, columns]'}")
+        rows, cols = got
+        step, unit = t.stride()
+        if rows <= 1:
+            step = max(cols, 1)
+        if (cols > 1 and unit != 1) or step < cols:
             raise ValueError(f"{name}: strides {t.stride()}: columns must be contiguous and rows must not overlap")
-        return t.data_ptr(), ld
+        return t.data_ptr(), step
 
     def _like_rows(self, t, ld):
         """An empty matrix with t's shape and row stride: where the logits' rows start on 16 bytes their gradient's do too."""
@@ -508,7 +523,7 @@ class Ops:
     def _dense(self, name, t, shape, dtype):
         if t is None:
             return 0
-        if t.dtype != dtype or not self._here(t) or tuple(t.shape) != shape or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not self._here(t):
             raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
@@ -535,8 +550,7 @@ class Ops:
         if out is None:
             t, at = self._scratch(n)
             out = LinearWeights(K, N, self.dt, t, at)
-        with torch.cuda.device(self.device):
-            hpf_op_linear_pack(ptr, K, N, out.ptr, n, self._s())
+        self._enqueue(hpf_op_linear_pack, ptr, K, N, out.ptr, n)
         return out
 
     def _weights(self, weights):
@@ -559,11 +573,10 @@ class Ops:
         y = out if out is not None else torch.empty((M, N), dtype=self.tdtype, device=self.device)
         yp, ldy = self._rows("out", y, (M, N))
         sl = torch.empty((M, N), dtype=self.tdtype, device=self.device) if slope and activation != "none" else None
-        with torch.cuda.device(self.device):
-            n = hpf_op_linear_workspace_bytes(self.dt, M, K, N)
-            ws, wsp = self._scratch(n)
-            hpf_op_linear_forward(self.dt, xp, ldx, wp, bp, rp, ldr, yp, ldy, sl.data_ptr() if sl is not None else 0, M, K, N,
-                                  ACTIVATIONS[activation], wsp, n, self._s())
+        n = hpf_op_linear_workspace_bytes(self.dt, M, K, N)
+        ws, wsp = self._scratch(n)
+        self._enqueue(hpf_op_linear_forward, self.dt, xp, ldx, wp, bp, rp, ldr, yp, ldy, sl.data_ptr() if sl is not None else 0, M, K, N,
+                      ACTIVATIONS[activation], wsp, n)
         return (y, sl) if slope else y
 
     def linear_backward(self, dy, x, weights, slope=None, need_dx=True, dw=None, db=None, accumulate=False):
@@ -582,11 +595,10 @@ class Ops:
         dw = torch.empty((K, N), dtype=torch.float32, device=self.device) if dw is None else dw
         db = torch.empty(N, dtype=torch.float32, device=self.device) if db is None else db
         dwp, dbp = self._dense("dw", dw, (K, N), torch.float32), self._dense("db", db, (N,), torch.float32)
-        with torch.cuda.device(self.device):
-            n = hpf_op_linear_workspace_bytes(self.dt, M, K, N)
-            ws, wsp = self._scratch(n)
-            hpf_op_linear_backward(self.dt, dyp, lddy, xp, ldx, wp, sp, dx.data_ptr() if need_dx else 0, K, dwp, dbp, accumulate,
-                                   M, K, N, wsp, n, self._s())
+        n = hpf_op_linear_workspace_bytes(self.dt, M, K, N)
+        ws, wsp = self._scratch(n)
+        self._enqueue(hpf_op_linear_backward, self.dt, dyp, lddy, xp, ldx, wp, sp, dx.data_ptr() if need_dx else 0, K, dwp, dbp, accumulate,
+                      M, K, N, wsp, n)
         return dx, dw, db
 
     def _labels(self, labels, rows):
@@ -599,15 +611,17 @@ class Ops:
         rows, classes = logits.shape
         lab = self._labels(labels, rows)
 
-        def new(*shape, dtype=torch.float32):
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        r = LogProb(new(rows) if labels is not None else None, new(rows), new(rows, dtype=torch.int32) if labels is not None else None,
-                    new(rows, 2), new(rows, top, dtype=torch.int32) if top > 0 else None, new(rows, top) if top > 0 else None)
-        with torch.cuda.device(self.device):
-            n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
-            ws, wsp = self._scratch(n)
-            p = [t.data_ptr() if t is not None else 0 for t in r]
-            hpf_op_logprob_forward(self.dt, lp, ld, lab, p[0], p[1], p[2], p[3], p[4], p[5], top, rows, classes, wsp, n, self._s())
+        f32, i32, dev, empty = torch.float32, torch.int32, self.device, torch.empty
+        has = labels is not None
+        r = LogProb(empty(rows, dtype=f32, device=dev) if has else None, empty(rows, dtype=f32, device=dev),
+                    empty(rows, dtype=i32, device=dev) if has else None, empty((rows, 2), dtype=f32, device=dev),
+                    empty((rows, top), dtype=i32, device=dev) if top > 0 else None,
+                    empty((rows, top), dtype=f32, device=dev) if top > 0 else None)
+        n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
+        ws, wsp = self._scratch(n)
+        self._enqueue(hpf_op_logprob_forward, self.dt, lp, ld, lab, r.logprob.data_ptr() if has else 0, r.entropy.data_ptr(),
+                      r.rank.data_ptr() if has else 0, r.stats.data_ptr(), r.top_index.data_ptr() if top > 0 else 0,
+                      r.top_logprob.data_ptr() if top > 0 else 0, top, rows, classes, wsp, n)
         return r
 
     def logprob_backward(self, logits, labels, stats, grad_logprob=None, entropy=None, grad_entropy=None, out=None):
@@ -618,10 +632,9 @@ class Ops:
         f32 = torch.float32
         d = out if out is not None else self._like_rows(logits, ld)
         dp, ldd = self._rows("out", d, (rows, classes))
-        with torch.cuda.device(self.device):
-            hpf_op_logprob_backward(self.dt, lp, ld, self._labels(labels, rows), self._dense("stats", stats, (rows, 2), f32),
-                                    self._dense("grad_logprob", grad_logprob, (rows,), f32), self._dense("entropy", entropy, (rows,), f32),
-                                    self._dense("grad_entropy", grad_entropy, (rows,), f32), dp, ldd, rows, classes, self._s())
+        self._enqueue(hpf_op_logprob_backward, self.dt, lp, ld, self._labels(labels, rows), self._dense("stats", stats, (rows, 2), f32),
+                      self._dense("grad_logprob", grad_logprob, (rows,), f32), self._dense("entropy", entropy, (rows,), f32),
+                      self._dense("grad_entropy", grad_entropy, (rows,), f32), dp, ldd, rows, classes)
         return d
 
     def distill(self, logits, top_index, top_logit, labels=None, temperature=1.0, hard_weight=0.0, row_weight=None, gradient=True):
@@ -635,12 +648,11 @@ class Ops:
         tl = self._dense("top_logit", top_logit, (rows, top), torch.float32)
         loss = torch.empty(rows, dtype=torch.float32, device=self.device)
         d = self._like_rows(logits, ld) if gradient else None
-        with torch.cuda.device(self.device):
-            n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
-            ws, wsp = self._scratch(n)
-            hpf_op_distill(self.dt, lp, ld, ti, tl, top, self._labels(labels, rows), temperature, hard_weight,
-                           self._dense("row_weight", row_weight, (rows,), torch.float32), loss.data_ptr(),
-                           d.data_ptr() if gradient else 0, ld, rows, classes, wsp, n, self._s())
+        n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
+        ws, wsp = self._scratch(n)
+        self._enqueue(hpf_op_distill, self.dt, lp, ld, ti, tl, top, self._labels(labels, rows), temperature, hard_weight,
+                      self._dense("row_weight", row_weight, (rows,), torch.float32), loss.data_ptr(), d.data_ptr() if gradient else 0, ld,
+                      rows, classes, wsp, n)
         return loss, d
 
 
