@@ -299,20 +299,26 @@ struct Held {
                                          (__attribute__((address_space(3))) void*)(room + j * NT + (t & ~63)), 16, 0, 0);
     }
   }
-  // AHEAD units per thread come from `room`, where fetch has brought them
-  template <int AHEAD = 0>
+  // unit j of a row, from memory (or from `room`); an end's unit is left to edge
+  __device__ __forceinline__ void load_unit(const T* p, int n, int t, int j, const uint4* room) {
+    constexpr uint32_t NONE = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    const int shift_ = (int)(((uintptr_t)p & 15) / sizeof(T)), u = t + j * NT;
+    const char* units = (const char*)(p - shift_);
+    uint4 q = make_uint4(NONE, NONE, NONE, NONE);
+    if (u >= (shift_ ? 1 : 0) && u < (shift_ + n) / E) q = room ? room[u] : *reinterpret_cast<const uint4*>(units + j * (NT * 16) + (unsigned)t * 16u);
+    v[j][0] = q.x; v[j][1] = q.y; v[j][2] = q.z; v[j][3] = q.w;
+  }
+  // Units j < AHEAD come from `room`, where fetch has brought them; units from DONE on are there already
+  template <int AHEAD = 0, int DONE = J>
   __device__ __forceinline__ void load(const T* p, int n, int t, const uint4* room = nullptr) {
     shift = (int)(((uintptr_t)p & 15) / sizeof(T));
     len = n;
     tid = t;
     constexpr uint32_t NONE = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-    const char* units = (const char*)(p - shift);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
+    for (int j = 0; j < DONE; ++j) {
       if (!used(j)) break;
-      uint4 q = make_uint4(NONE, NONE, NONE, NONE);
-      if (inside(j)) q = j < AHEAD ? room[t + j * NT] : *reinterpret_cast<const uint4*>(units + j * (NT * 16) + (unsigned)t * 16u);
-      v[j][0] = q.x; v[j][1] = q.y; v[j][2] = q.z; v[j][3] = q.w;
+      load_unit(p, n, t, j, j < AHEAD ? room : nullptr);
     }
     const int whole = (shift + n) / E;
     if (shift) edge(p, 0, NONE);
@@ -349,9 +355,9 @@ struct Held {
       for (int w = 0; w < 4; ++w) asm("" : "+v"(v[j][w]));
   }
   // Every element's f(value, j, e) to the same element of d.  Where d's elements do not have the same places within 16 bytes they are stored
-  // one by one.
-  template <class F>
-  __device__ __forceinline__ void store(T* d, F f) {
+  // one by one.  after(j): called when unit j is out of the way.
+  template <class F, class G>
+  __device__ __forceinline__ void store(T* d, F f, G after) {
     const bool alike = (int)(((uintptr_t)d & 15) / sizeof(T)) == shift;
     const int whole = (shift + len) / E;
     char* units = (char*)(d - shift);
@@ -376,6 +382,7 @@ struct Held {
         for (int e = 0; e < E; ++e)
           if (e0 + e >= 0 && e0 + e < len) from_f32(at + e, x[e]);
       }
+      after(j);
     }
   }
   // f(value, j, e) for all units in use
@@ -731,7 +738,7 @@ __global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a, uns
     return m == -INF ? 0.f : fmaf(ngh * p, fmaxf(logp, -120.f) + entropy, ng * expm1f(logp));
   };
   const int at_label = label - (int)c0;
-  h.store(d + c0, [&](float x, int j, int e) { return grad(x); });
+  h.store(d + c0, [&](float x, int, int) { return grad(x); }, [](int) {});
   // the label's, once more
   const int unit = (at_label + h.shift) / H::E;
   if (label >= 0 && label < a.classes && at_label >= 0 && at_label < h.len && unit % 256 == h.tid) {
@@ -915,8 +922,8 @@ struct Answer {
 };
 
 // gradient of the `len` held elements to d
-template <int HARD, class T, int NT, int J>
-__device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero) {
+template <int HARD, class T, int NT, int J, class G>
+__device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero, G after) {
   const Exponents x(m, it);
   h.renew();
   h.store(d, [&](float s, int, int) {
@@ -924,7 +931,7 @@ __device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m,
     float y = fs * e;
     if (HARD) y = fmaf(fh, x.hard<HARD>(s, e), y);
     return zero ? 0.f : y;
-  });
+  }, after);
 }
 
 // A row that a group holds whole
@@ -947,7 +954,7 @@ __device__ __forceinline__ void distill_row(const Distill& a, const Group<NT>& g
   T* d = (T*)a.dlogits + row * a.ldd;
   typename Answer<T>::Entries entries{-1, -1, 0.f, 0.f};
   if (g.tid < 64) entries = ans.entries(l, g.tid);
-  write_gradient<HARD>(h, d, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad);
+  write_gradient<HARD>(h, d, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad, [](int) {});
   if (NT > 64) __syncthreads(); else __builtin_amdgcn_s_waitcnt(0x0f70);   // the stores above are done before the entries replace some of them
   if (g.tid < 64) Answer<T>::write(entries, d, 0, a.classes);
 }
@@ -966,7 +973,7 @@ __global__ __launch_bounds__(NT * PER) void k_distill(Distill a) {
   if (g.tid < 64) l = read_list(a, s, row, g.tid);
   distill_row<HARD>(a, g, h, ans, l, row);
 }
-// Long rows, like k_logprob_rows.  Loss and entries are left to k_distill_entries, which finds the rows' sums in `records`: their double
+// Long rows, like k_logprob_rows; the units that LDS has no room for follow into their registers as the gradient leaves them.  Loss and entries are left to k_distill_entries, which finds the rows' sums in `records`: their double
 // arithmetic next to a row in registers costs more registers than there are.
 template <int HARD, class T, int J, int AHEAD>
 __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records) {
@@ -977,12 +984,16 @@ __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records)
   const float it = 1.f / a.temperature;
   int row = blockIdx.x;
   const T* s = (const T*)a.logits + row * a.ld;
+  H h;
   H::template fetch<AHEAD>(s, a.classes, g.tid, room);
+#pragma unroll
+  for (int j = AHEAD; j < J; ++j) h.load_unit(s, a.classes, g.tid, j, nullptr);
+  __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): the thread's units are in LDS
   for (; row < a.rows; row += gridDim.x) {
     s = (const T*)a.logits + row * a.ld;
-    H h;
-    __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the thread's units are in LDS
-    h.template load<AHEAD>(s, a.classes, g.tid, room);
+    const bool more = row + (int)gridDim.x < a.rows;
+    const T* next = s + gridDim.x * a.ld;
+    h.template load<AHEAD, AHEAD < J ? AHEAD : J>(s, a.classes, g.tid, room);
     const int label = label_of(a.labels, row);
     const bool has = label >= 0 && label < a.classes;
     const float w = a.row_weight ? a.row_weight[row] : 1.f;
@@ -993,15 +1004,22 @@ __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records)
       if (g.tid == 0) space.n = (int)some | (int)broken << 1;
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): they are read
-    if (row + (int)gridDim.x < a.rows) H::template fetch<AHEAD>(s + gridDim.x * a.ld, a.classes, g.tid, room);
+    if (more) H::template fetch<AHEAD>(next, a.classes, g.tid, room);
     const Soft v = soft_of<HARD>(g, h, it);
     const bool some = space.n & 1, empty = v.m == -INF;
     const bool bad = v.m == INF || v.restt != v.restt || (HARD && v.rest1 != v.rest1) || (space.n & 2) || (label != -1 && !has);
     if (g.tid == 0) records[row] = v;
+    __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the next row's units are in LDS; before the stores, whose end nobody awaits
+    auto after = [&](int j) { if (j >= AHEAD && more) h.load_unit(next, a.classes, g.tid, j, nullptr); };
     if (a.dlogits) {
       const float fs = bad ? quiet_nan() : some ? w * (1.f - a.hard_weight) * a.temperature / (1.f + v.restt) : 0.f;
       const float fh = bad ? quiet_nan() : HARD && has ? w * a.hard_weight / (1.f + v.rest1) : 0.f;
-      write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, fs, fh, empty && !bad);
+      write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, fs, fh, empty && !bad, after);
+    }
+    if (!a.dlogits || !h.used(J - 1)) {                // units that this row does not have, but the next may
+#pragma unroll
+      for (int j = AHEAD; j < J; ++j)
+        if (!a.dlogits || !h.used(j)) after(j);
     }
     __syncthreads();                                   // space.n is read
   }
@@ -1076,7 +1094,7 @@ __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long
     step = c_end - c0 < room ? c_end - c0 : room;
     H h;
     h.load(s + c0, (int)step, tid);
-    write_gradient<HARD>(h, d + c0, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad);
+    write_gradient<HARD>(h, d + c0, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad, [](int) {});
   }
   __syncthreads();
   if (tid < 64) Answer<T>::write(ans.entries(l, tid), d, c_begin, c_end);
