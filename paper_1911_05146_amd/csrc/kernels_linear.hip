@@ -139,12 +139,14 @@ __global__ __launch_bounds__(512) void k_linear_tile_f32(Operand A, Operand B, E
 
 // ---- bf16: tiles on matrix cores -------------------------------------------------------------------------------------
 // C[m][n] = sum_k A[m][k] B[n][k], both operands with k contiguous, rows on 16 bytes; k >= K counts as 0 in A, and B's rows are padded
-// with zeros to a multiple of 64.
+// with zeros to a multiple of 64.  ROWS: C[m][n] = sum_k A[k][m] B[k][n], the contraction over the operands' rows (dw = x^T dz), k >= K
+// counts as 0 in both; M and N as wide as the rows, multiples of 8 that may count columns beyond the result's.
 enum : int { OUT_Y = 0, OUT_SUM = 1, OUT_SLAB = 2 };
 struct Product {
   const bf16_t* A; long lda;
   const bf16_t* B; long ldb;
   int M, N, K;
+  int widthA, widthB;           // ROWS: readable columns
   // OUT_Y
   const float* bias;
   const bf16_t* residual; long ldr;
@@ -282,6 +284,16 @@ __device__ __forceinline__ void tile_of(unsigned i, unsigned rows, unsigned cols
 // s_waitcnt vmcnt(n), and lgkmcnt(0) with it
 constexpr int wait_loads(int n) { return 0x0070 | (n & 15) | (n >> 4) << 14; }
 
+// 16 bytes per lane from memory to LDS, lane i's to lds + 16 i; lds: byte address, the same in all lanes.  Written out because the compiler, which
+// knows the builtin as a write to LDS, lets every read that it cannot tell apart from it (ds_read_b64_tr_b16 for one) wait for all of them:
+// 416 instead of 200 us for dw of 4096 x 4096 from 8192 rows.  Nothing is returned in registers; who reads has waited (wait_loads, a barrier).
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char* base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "m0");
+}
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char* at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(at) : "m0");
+}
+
 // A barrier that no access to LDS is moved across; what has to be waited for, the caller waits for
 __device__ __forceinline__ void stage_barrier() {
   asm volatile("" ::: "memory");
@@ -295,7 +307,12 @@ __device__ __forceinline__ void stage_barrier() {
 // barrier, behind which the next stage is complete and this one free; among the products of the second half, the loads of a later step
 // go out into it and the first fragments of the next step are read.  Issued in one burst instead, these reads and loads kept the matrix
 // cores waiting: 213 instead of 200 us at 8192 x 4096 x 4096 (1370 TFLOP/s; 4096 x 8192 x 4096, one tile per CU: 1440).
-template <int BM, int BN, int WM, int WN, int STAGES, int OUT>
+//
+// ROWS: a stage is 64 rows of BM and of BN columns, and ds_read_b64_tr_b16 turns them on the way into the registers: from four rows' 4 x 16
+// elements every lane of 16 gets a column's four.  The 32-byte pieces of a row are stored in the order piece ^ f(row), with f over the 16 rows
+// of a read such that no more than two of them share banks, and two trips are what 512 bytes take anyway.  Turned copies of both operands
+// instead cost a pass over each: 75 us at 8192 x 4096 x 4096, of which 33 remain for dz = dy * slope.
+template <int BM, int BN, int WM, int WN, int STAGES, int OUT, bool ROWS>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigned tile_rows, unsigned tile_cols, int steps_per_split) {
   constexpr int NT = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * 64;
   constexpr int LA = BM * 8 / NT, LB = BN * 8 / NT;      // 16-byte units per thread and step
@@ -309,31 +326,45 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
   const int steps = (k_all - k_begin < steps_per_split ? k_all - k_begin : steps_per_split);
 
   // thread: rows tid / 8 + i * NT / 8, unit tid % 8 of the stage, which holds unit (tid ^ row) % 8 of the operand.  Rows behind the last one read
-  // the last one; offsets within a tile fit 32 bits (256 rows of 2^20).
+  // the last one; offsets within a tile fit 32 bits (256 rows, 2^22 apart at most).
   const int unit = (tid ^ (tid >> 3)) & 7;
   uint32_t oa[LA], ob[LB];
+  // ROWS: thread's unit i is unit i * NT + tid of the stage, rows of W / 8 units; columns behind the last one read the last ones.  Its units are a
+  // multiple of 16 rows apart, in the same column, so that one offset serves all.
+  auto piece = [](int r, int W) { return W == 64 ? (r >> 1 & 1) | (r >> 3 & 1) << 1 : (r & 3) | (r >> 3 & 1) << 2; };
+  static_assert(NT * 8 / BM % 16 == 0 && NT * 8 / BN % 16 == 0, "a thread's units share their column");
+  auto at_rows = [&](int W, long ld, int first, int width) {
+    const int r = tid / (W / 8), c = tid % (W / 8);
+    int col = first + (((c >> 1 ^ piece(r, W)) << 1 | (c & 1)) << 3);
+    if (col > width - 8) col = width - 8;
+    return (uint32_t)(r * ld + col) * 2u;
+  };
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
     const int r = (tid >> 3) + i * (NT / 8), last = p.M - 1 - m0;
-    oa[i] = (uint32_t)((r < last ? r : last) * p.lda + unit * 8) * 2u;
+    oa[i] = ROWS ? at_rows(BM, p.lda, m0, p.widthA) : (uint32_t)((r < last ? r : last) * p.lda + unit * 8) * 2u;
   }
 #pragma unroll
   for (int i = 0; i < LB; ++i) {
     const int r = (tid >> 3) + i * (NT / 8), last = p.N - 1 - n0;
-    ob[i] = (uint32_t)((r < last ? r : last) * p.ldb + unit * 8) * 2u;
+    ob[i] = ROWS ? at_rows(BN, p.ldb, n0, p.widthB) : (uint32_t)((r < last ? r : last) * p.ldb + unit * 8) * 2u;
   }
-  const char* ga = (const char*)(p.A + m0 * p.lda + k_begin * 64);
-  const char* gb = (const char*)(p.B + n0 * p.ldb + k_begin * 64);
+  const char* ga = (const char*)(ROWS ? p.A + (long)k_begin * 64 * p.lda : p.A + m0 * p.lda + k_begin * 64);
+  const char* gb = (const char*)(ROWS ? p.B + (long)k_begin * 64 * p.ldb : p.B + n0 * p.ldb + k_begin * 64);
+  const long step_a = ROWS ? 128 * p.lda : 128, step_b = ROWS ? 128 * p.ldb : 128;        // bytes
   const int k_left = p.K - k_begin * 64;
+  const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem) + (uint32_t)wave * 1024u;
   auto load_unit = [&](int step, int i, bool ends) {     // unit i < LA of A, then those of B; ends: the contraction ends within this step
-    bf16_t* s = smem + (step % STAGES) * STAGE + wave * 512;
-    if (i < LA) {
-      const char* a = ga + step * 128 + oa[i < LA ? i : 0];
-      if (ends && k_left <= step * 64 + unit * 8) a = (const char*)kZeros;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)a, (__attribute__((address_space(3))) void*)(s + i * (NT * 8)), 16, 0, 0);
+    const uint32_t s = lds0 + (uint32_t)(step % STAGES) * (STAGE * 2) + (uint32_t)i * (NT * 16);      // B's units follow A's
+    const bool of_a = i < LA;
+    const char* base = of_a ? ga + step * step_a : gb + step * step_b;
+    if (ROWS) base += of_a ? i * (NT * 8 / BM) * 2 * p.lda : (i - LA) * (NT * 8 / BN) * 2 * p.ldb;
+    const uint32_t offset = of_a ? oa[of_a ? i : 0] : ob[of_a ? 0 : i - LA];
+    if (ends && (of_a || ROWS)) {
+      const int k = ROWS ? of_a ? (i * NT + tid) / (BM / 8) : ((i - LA) * NT + tid) / (BN / 8) : unit * 8;
+      load_to_lds(s, k_left <= step * 64 + k ? (const char*)kZeros : base + offset);
     } else {
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(gb + step * 128 + ob[i < LA ? 0 : i - LA]),
-                                       (__attribute__((address_space(3))) void*)(s + BM * 64 + (i - LA) * (NT * 8)), 16, 0, 0);
+      load_to_lds(s, base, offset);
     }
   };
   auto load = [&](int step) {
@@ -349,10 +380,23 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
 
   const int row = lane & 15, q = lane >> 4;
   const int at_a = (wm * (BM / WM) + row) * 64, at_b = BM * 64 + (wn * (BN / WN) + row) * 64;
-  const int u0 = ((q) ^ (row & 7)) * 8, u1 = ((q + 4) ^ (row & 7)) * 8;
+  const int u0 = ROWS ? 0 : ((q) ^ (row & 7)) * 8, u1 = ROWS ? 32 : ((q + 4) ^ (row & 7)) * 8;
   struct Frags { bf16x8 a[TM], b[TN]; };
-  auto read_one = [&](Frags& f, int step, int u, int i) {
+  // ROWS: the lane's place in a stage of either operand, its piece not yet taken in
+  const int tr_row = q * 8 + (row >> 2), tr_a = tr_row * BM + piece(tr_row, BM) * 16 + (row & 3) * 4, tr_b = tr_row * BN + piece(tr_row, BN) * 16 + (row & 3) * 4;
+  auto read_turned = [&](const bf16_t* s, int at, int W) {       // 8 rows of 16 columns
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s4 lds_s4;
+    struct Pair { s4 lo, hi; } v = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + at)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(s + at + 4 * W))};
+    return __builtin_bit_cast(bf16x8, v);
+  };
+  auto read_one = [&](Frags& f, int step, int u, int i) {        // u: u0 or u1; ROWS: 0 or 32, the first row of the half
     const bf16_t* s = smem + (step % STAGES) * STAGE;
+    if (ROWS) {
+      if (i < TN) f.b[i < TN ? i : 0] = read_turned(s + BM * 64 + u * BN, tr_b ^ (wn * (BN / WN) + i * 16), BN);
+      else f.a[i < TN ? 0 : i - TN] = read_turned(s + u * BM, tr_a ^ (wm * (BM / WM) + (i - TN) * 16), BM);
+      return;
+    }
     if (i < TN) f.b[i < TN ? i : 0] = *reinterpret_cast<const bf16x8*>(s + at_b + i * 1024 + u);
     else f.a[i < TN ? 0 : i - TN] = *reinterpret_cast<const bf16x8*>(s + at_a + (i - TN) * 1024 + u);
   };
@@ -412,28 +456,28 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
 
   // A wave's results go through its own part of LDS, 16 rows at a time, so that a lane ends up with 8 consecutive columns
   constexpr int TS = BN / WN + 4;                        // fp32 row stride: rows shift by 4 banks
-  constexpr int LANES = BN / WN / 8, ROWS = 64 / LANES;  // lanes per row, rows per pass
+  constexpr int LANES = BN / WN / 8, PASS = 64 / LANES;  // lanes per row, rows per pass
   static_assert(16 * TS * 4 * WM * WN <= STAGES * STAGE * 2, "the rows of all waves fit the stages");
   float* mine = reinterpret_cast<float*>(smem) + wave * 16 * TS;
   const int n = n0 + wn * (BN / WN) + (lane % LANES) * 8, m_lane = m0 + wm * (BM / WM) + lane / LANES;
   const Ahead a = ahead<OUT>(p, n);
-  uint4 res[TM][16 / ROWS];
+  uint4 res[TM][16 / PASS];
   if (OUT == OUT_Y && p.residual)
 #pragma unroll
     for (int j = 0; j < TM; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; r += ROWS) res[j][r / ROWS] = residual8<OUT>(p, m_lane + j * 16 + r, n);
+      for (int r = 0; r < 16; r += PASS) res[j][r / PASS] = residual8<OUT>(p, m_lane + j * 16 + r, n);
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
 #pragma unroll
     for (int i = 0; i < TN; ++i) *reinterpret_cast<floatx4*>(mine + row * TS + i * 16 + q * 4) = acc[i][j];
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int r = 0; r < 16; r += ROWS) {
+    for (int r = 0; r < 16; r += PASS) {
       const int m = m_lane + j * 16 + r;
       float v[8];
       load8(mine + (r + lane / LANES) * TS + (lane % LANES) * 8, v);
-      if (m < p.M && n < p.N) finish8<OUT>(p, m, n, v, blockIdx.y, a, res[j][r / ROWS]);
+      if (m < p.M && n < p.N) finish8<OUT>(p, m, n, v, blockIdx.y, a, res[j][r / PASS]);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -509,121 +553,71 @@ __global__ __launch_bounds__(256) void k_linear_join(Product p, const float* __r
   }
 }
 
-// Rows that do not start on 16 bytes or are no multiple of 8 long: copied to [M][ld], zeros behind the end
-__global__ __launch_bounds__(256) void k_linear_rows(const bf16_t* __restrict__ src, long lds, bf16_t* __restrict__ dst, int ld, int M, int K) {
-  const int units = ld / 8;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)M * units; i += (size_t)gridDim.x * 256) {
-    const int m = (int)(i / units), k = (int)(i - (size_t)m * units) * 8;
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (k + e < K) w[e >> 1] |= (uint32_t)src[m * lds + k + e] << (16 * (e & 1));
-    *reinterpret_cast<uint4*>(dst + (size_t)m * ld + k) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
-
-// Transposed copy turned[c][m] of src[m][c] (* slope), rows padded with zeros to ld, for the product whose contraction runs over the rows; with
-// rows: also the product itself, rows padded to rld; with sums: column sums of each 256 rows.  A wave has 64 x 64 elements, a lane 8 x 8 of
-// them: it loads 8 units of 16 bytes, turns them in registers and stores 8, and both sides have 128 contiguous bytes per 8 lanes.
-struct Turn {
+// dst = src (* slope), rows padded with zeros to ld, and the column sums of each group of rows; either may be missing.  A wave takes 512 columns
+// of a row, four rows on their way at a time; its lanes have columns of their own, so sums need no exchange but that of the four waves.  A second
+// operand's copy rides along.  dz and its sums at 8192 x 4096: 46 us (4.4 TB/s).
+struct Rows {
   const bf16_t* src; long lds;
   const bf16_t* slope;          // dense
-  bf16_t* turned; int ld;
-  bf16_t* rows; int rld;
-  float* sums;
-  int M, cols, wide;            // wide: src (and slope) rows allow 16-byte loads
-  unsigned col_blocks, blocks;
+  bf16_t* dst; int ld;
+  float* sums;                  // [M / group][cols]
+  int M, cols, wide;            // wide: src and slope rows allow 16-byte loads
+  int group;                    // rows of a work-group, a multiple of 16
 };
-// eight rows of eight bf16 -> eight columns: pairs, then pairs of pairs, then the two halves
-__device__ __forceinline__ void turn8(uint32_t (&r)[8][4]) {
-  uint32_t t[8][4];
-#pragma unroll
-  for (int i = 0; i < 8; i += 2)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      t[i][w] = __builtin_amdgcn_perm(r[i + 1][w], r[i][w], 0x05040100);       // element 2w of rows i, i + 1
-      t[i + 1][w] = __builtin_amdgcn_perm(r[i + 1][w], r[i][w], 0x07060302);   // element 2w + 1
-    }
-#pragma unroll
-  for (int c = 0; c < 8; ++c)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) r[c][w] = t[2 * w + (c & 1)][c >> 1];
-}
-__global__ __launch_bounds__(256) void k_linear_turn(Turn first, Turn second) {
-  const bool two = blockIdx.x >= first.blocks;
-  const Turn& p = two ? second : first;
-  const unsigned b = two ? blockIdx.x - first.blocks : blockIdx.x;
+__global__ __launch_bounds__(256) void k_linear_rows(Rows first, Rows second, unsigned blocks) {       // blocks: of first
+  __shared__ float part[4][512];
+  const bool one = blockIdx.x < blocks;
+  const Rows p = one ? first : second;
+  const unsigned block = one ? blockIdx.x : blockIdx.x - blocks, col_blocks = (unsigned)(p.ld + 511) / 512;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int cb = lane & 7, mb = lane >> 3;
-  const int c0 = (int)(b % p.col_blocks) * 64, g = (int)(b / p.col_blocks), m0 = g * 256 + wave * 64;
-  const int c = c0 + cb * 8, m = m0 + mb * 8;
-  uint32_t r[8][4];
-  if (p.wide) {                 // cols is a multiple of 8
+  const int g = (int)(block / col_blocks), c0 = (int)(block % col_blocks) * 512, c = c0 + lane * 8;
+  float sum[8] = {};
+  auto fetch = [&](const bf16_t* r, int m, uint32_t (&w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint4 q = make_uint4(0u, 0u, 0u, 0u);
-      if (m + i < p.M && c < p.cols) q = *reinterpret_cast<const uint4*>(p.src + (m + i) * p.lds + c);
-      r[i][0] = q.x; r[i][1] = q.y; r[i][2] = q.z; r[i][3] = q.w;
+    for (int i = 0; i < 4; ++i) w[i] = 0;
+    if (m >= p.M || c >= p.cols) return;
+    if (p.wide) {               // cols is a multiple of 8
+      const uint4 q = *reinterpret_cast<const uint4*>(r + c);
+      w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < p.cols) w[e >> 1] |= (uint32_t)r[c + e] << (16 * (e & 1));
     }
-  } else {
+  };
+  const int each = p.group / 4, m0 = g * p.group + wave * each;
+  for (int i0 = 0; i0 < each; i0 += 4) {
+    uint32_t r[4][4], s[4][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i) {
+      const long m = m0 + i0 + i;
+      fetch(p.src + m * p.lds, (int)m, r[i]);
+      if (p.slope) fetch(p.slope + m * p.cols, (int)m, s[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = m0 + i0 + i;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        r[i][w] = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (m + i < p.M && c + w * 2 + h < p.cols) r[i][w] |= (uint32_t)p.src[(m + i) * p.lds + c + w * 2 + h] << (16 * h);
+        if (p.slope)            // exact in fp32, then one rounding
+          r[i][w] = pack_bf16x2(__uint_as_float(r[i][w] << 16) * __uint_as_float(s[i][w] << 16),
+                                __uint_as_float(r[i][w] & 0xffff0000u) * __uint_as_float(s[i][w] & 0xffff0000u));
+        sum[2 * w] += __uint_as_float(r[i][w] << 16);
+        sum[2 * w + 1] += __uint_as_float(r[i][w] & 0xffff0000u);
       }
-  }
-  if (p.slope) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint32_t s[4] = {0, 0, 0, 0};
-      if (p.wide) {
-        if (m + i < p.M && c < p.cols) {
-          const uint4 q = *reinterpret_cast<const uint4*>(p.slope + (size_t)(m + i) * p.cols + c);
-          s[0] = q.x; s[1] = q.y; s[2] = q.z; s[3] = q.w;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (m + i < p.M && c + e < p.cols) s[e >> 1] |= (uint32_t)p.slope[(size_t)(m + i) * p.cols + c + e] << (16 * (e & 1));
-      }
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        r[i][w] = pack_bf16x2(__uint_as_float(r[i][w] << 16) * __uint_as_float(s[w] << 16), __uint_as_float(r[i][w] & 0xffff0000u) * __uint_as_float(s[w] & 0xffff0000u));
+      if (p.dst && m < p.M && c < p.ld) *reinterpret_cast<uint4*>(p.dst + (size_t)m * p.ld + c) = make_uint4(r[i][0], r[i][1], r[i][2], r[i][3]);
     }
   }
-  if (p.rows && c < p.rld)
+  if (!p.sums) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (m + i < p.M) *reinterpret_cast<uint4*>(p.rows + (size_t)(m + i) * p.rld + c) = make_uint4(r[i][0], r[i][1], r[i][2], r[i][3]);
-  if (p.sums) {
-    __shared__ float part[4][64];
-    float s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      s[e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[e] += __uint_as_float(e & 1 ? r[i][e >> 1] & 0xffff0000u : r[i][e >> 1] << 16);
-      for (int o = 8; o < 64; o <<= 1) s[e] += __shfl_xor(s[e], o);
-    }
-    if (mb == 0)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) part[wave][cb * 8 + e] = s[e];
-    __syncthreads();
-    if (wave == 0 && c0 + lane < p.cols)
-      p.sums[(size_t)g * p.cols + c0 + lane] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-  }
-  if (p.turned && m < p.ld) {
-    turn8(r);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < p.cols) *reinterpret_cast<uint4*>(p.turned + (size_t)(c + e) * p.ld + m) = make_uint4(r[e][0], r[e][1], r[e][2], r[e][3]);
+  for (int e = 0; e < 8; ++e) part[wave][lane + 64 * e] = sum[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 512; i += 256) {
+    const int n = c0 + (i & 63) * 8 + (i >> 6);
+    if (n < p.cols) p.sums[(size_t)g * p.cols + n] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
   }
 }
-// db from the sums of all groups of 256 rows, one order: 16 shares of the groups, then their sums
+// db from the sums of all groups of rows, one order: 16 shares of the groups, then their sums
 __global__ __launch_bounds__(1024) void k_linear_db_join(const float* __restrict__ sums, int groups, float* __restrict__ db, int accumulate, int N) {
   __shared__ float part[16][64];
   const int c = threadIdx.x & 63, w = threadIdx.x >> 6, n = blockIdx.x * 64 + c;
@@ -704,10 +698,10 @@ struct Cut {
   int kind, splits, steps;      // steps (of 64, CUT_FEW: 32) per share
   unsigned rows, cols;          // tiles
 };
-Cut cut_of(int M, int N, int K) {
+Cut cut_of(int M, int N, int K, bool rows) {      // rows: of a ROWS product
   auto tiles = [&](int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   Cut c;
-  c.kind = M <= 16 ? CUT_FEW : tiles(256, 256) >= 192 ? CUT_LARGE : tiles(128, 128) >= 256 ? CUT_TILES : CUT_SPLIT;
+  c.kind = M <= 16 && !rows ? CUT_FEW : tiles(256, 256) >= 192 ? CUT_LARGE : tiles(128, 128) >= 256 ? CUT_TILES : CUT_SPLIT;
   const int bm = c.kind == CUT_FEW ? 16 : c.kind == CUT_LARGE ? 256 : c.kind == CUT_TILES ? 128 : 64, bn = bm;
   c.rows = (unsigned)((M + bm - 1) / bm);
   c.cols = (unsigned)((N + bn - 1) / bn);
@@ -719,15 +713,15 @@ Cut cut_of(int M, int N, int K) {
   c.splits = (k + c.steps - 1) / c.steps;
   return c;
 }
-size_t slab_bytes(int M, int N, int K) {
-  const Cut c = cut_of(M, N, K);
+size_t slab_bytes(int M, int N, int K, bool rows) {
+  const Cut c = cut_of(M, N, K, rows);
   return c.splits > 1 ? align256((size_t)c.splits * M * slab_row(N) * sizeof(float)) : 0;
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, int OUT>
+template <int BM, int BN, int WM, int WN, int STAGES, int OUT, bool ROWS>
 hipError_t mfma(const Product& p, const Cut& c, hipStream_t s) {
   constexpr int lds = STAGES * (BM + BN) * 64 * 2;
-  const auto kernel = k_linear_mfma<BM, BN, WM, WN, STAGES, OUT>;
+  const auto kernel = k_linear_mfma<BM, BN, WM, WN, STAGES, OUT, ROWS>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
@@ -741,93 +735,109 @@ hipError_t few(const Product& p, const Cut& c, hipStream_t s) {
   return hipGetLastError();
 }
 
-// OUT: OUT_Y or OUT_SUM; slabs: room for slab_bytes
-template <int OUT>
+// y, or (ROWS) a sum; slabs: room for slab_bytes
+template <bool ROWS>
 hipError_t product(const Product& p, float* slabs, hipStream_t s) {
-  const Cut c = cut_of(p.M, p.N, p.K);
-  if (c.kind == CUT_LARGE) return mfma<256, 256, 2, 4, 2, OUT>(p, c, s);
-  if (c.kind == CUT_TILES) return mfma<128, 128, 2, 2, 2, OUT>(p, c, s);
-  if (c.splits == 1) return c.kind == CUT_FEW ? few<OUT>(p, c, s) : mfma<64, 64, 2, 2, 4, OUT>(p, c, s);
+  constexpr int OUT = ROWS ? OUT_SUM : OUT_Y;
+  const Cut c = cut_of(p.M, p.N, p.K, ROWS);
+  if (c.kind == CUT_LARGE) return mfma<256, 256, 2, 4, 2, OUT, ROWS>(p, c, s);
+  if (c.kind == CUT_TILES) return mfma<128, 128, 2, 2, 2, OUT, ROWS>(p, c, s);
+  if (c.splits == 1) {
+    if constexpr (!ROWS)
+      if (c.kind == CUT_FEW) return few<OUT>(p, c, s);
+    return mfma<64, 64, 2, 2, 4, OUT, ROWS>(p, c, s);
+  }
   Product q = p;
   q.sum = slabs;
-  const hipError_t e = c.kind == CUT_FEW ? few<OUT_SLAB>(q, c, s) : mfma<64, 64, 2, 2, 4, OUT_SLAB>(q, c, s);
+  hipError_t e;
+  if (!ROWS && c.kind == CUT_FEW) e = few<OUT_SLAB>(q, c, s);
+  else e = mfma<64, 64, 2, 2, 4, OUT_SLAB, ROWS>(q, c, s);
   if (e != hipSuccess) return e;
   k_linear_join<OUT><<<grid_for((size_t)p.M * ((p.N + 7) / 8), 256, 2048), 256, 0, s>>>(p, slabs, c.splits);
   return hipGetLastError();
 }
 
-bool direct(const void* p, long ld, int K) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (K & 7) == 0; }
+// Rows that the tiles read where they are: 16-byte units, and 256 rows within 32-bit offsets
+bool direct(const void* p, long ld, int K) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (K & 7) == 0 && ld <= 1 << 22; }
+
+// Rows in a work-group of k_linear_rows: 64, or 16 while that gives no CU two work-groups (1021 x 1000: 11.6 with 64, ROWS16 us with 16)
+int group_of(int M, int width) { return (long)((M + 63) / 64) * ((width + 511) / 512) >= 512 ? 64 : 16; }
+unsigned row_blocks(const Rows& r) { return (unsigned)((r.M + r.group - 1) / r.group) * (unsigned)((r.ld + 511) / 512); }
+// a copy whose rows start on 16 bytes
+Rows copy_of(const void* x, long ldx, int M, int K, char* to) {
+  const int Kp = round_up64(K);
+  return Rows{(const bf16_t*)x, ldx, nullptr, (bf16_t*)to, Kp, nullptr, M, K, 0, group_of(M, Kp)};
+}
 
 hipError_t forward_bf16(const LinearForward& a, char* ws, hipStream_t s) {
   Product p{};
   p.A = (const bf16_t*)a.x; p.lda = a.ldx; p.M = a.M; p.N = a.N; p.K = a.K;
   if (!direct(a.x, a.ldx, a.K)) {
-    const int ld = round_up64(a.K);
-    k_linear_rows<<<grid_for((size_t)a.M * ld / 8, 256, 4096), 256, 0, s>>>((const bf16_t*)a.x, a.ldx, (bf16_t*)ws, ld, a.M, a.K);
+    const Rows r = copy_of(a.x, a.ldx, a.M, a.K, ws);
+    k_linear_rows<<<row_blocks(r), 256, 0, s>>>(r, r, row_blocks(r));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    p.A = (const bf16_t*)ws; p.lda = ld; p.K = ld;
+    p.A = r.dst; p.lda = p.K = r.ld;
   }
   ws += align256((size_t)a.M * round_up64(a.K) * 2);
   p.B = (const bf16_t*)a.weights; p.ldb = round_up64(a.K);
   p.bias = a.bias; p.residual = (const bf16_t*)a.residual; p.ldr = a.ldr; p.y = (bf16_t*)a.y; p.ldy = a.ldy; p.slope = (bf16_t*)a.slope; p.act = a.act;
-  return product<OUT_Y>(p, (float*)ws, s);
+  return product<false>(p, (float*)ws, s);
 }
 
-Turn turn_of(const void* src, long lds, const void* slope, int M, int cols, bf16_t* turned, int ld, bf16_t* rows, int rld, float* sums) {
-  Turn t{(const bf16_t*)src, lds, (const bf16_t*)slope, turned, ld, rows, rld, sums, M, cols, 0, 0, 0};
-  t.wide = direct(src, lds, cols) && ((uintptr_t)slope & 15) == 0;
-  t.col_blocks = blocks64(cols);
-  t.blocks = t.col_blocks * (unsigned)((M + 255) / 256);
-  return t;
-}
-
-// Workspace of a backward call: dz [M][Np] | dz^T [N][Mp] | x^T [K][Mp] | sums of 256 rows [M/256][N] | shares of a split product
+// Workspace of a backward call: dz [M][Np] | x [M][Kp] | sums of groups of rows [groups][N] | shares of a split product
 struct BackwardSpace {
-  size_t dz, dzt, xt, sums, slabs, bytes;
+  size_t dz, x, sums, slabs, bytes;
+  int group, groups;            // rows of a sum; sums
   BackwardSpace(int M, int K, int N) {
-    const size_t Mp = round_up64(M), Np = round_up64(N);
+    const size_t Kp = round_up64(K), Np = round_up64(N);
     dz = 0;
-    dzt = align256((size_t)M * Np * 2);
-    xt = dzt + align256((size_t)N * Mp * 2);
-    sums = xt + align256((size_t)K * Mp * 2);
-    slabs = sums + align256((size_t)((M + 255) / 256) * N * 4);
-    const size_t d = slab_bytes(M, K, (int)Np), w = slab_bytes(K, N, (int)Mp);
+    group = group_of(M, (int)Np);
+    groups = (M + group - 1) / group;
+    x = align256((size_t)M * Np * 2);
+    sums = x + align256((size_t)M * Kp * 2);
+    slabs = sums + align256((size_t)groups * N * 4);
+    const size_t d = slab_bytes(M, K, (int)Np, false), w = slab_bytes(K, N, M, true);
     bytes = slabs + (d > w ? d : w);
   }
 };
 
 hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
   const BackwardSpace at(a.M, a.K, a.N);
-  const int Mp = round_up64(a.M), Np = round_up64(a.N);
-  const bool copy = a.dx && (a.slope || !direct(a.dy, a.lddy, a.N));
-  bf16_t* dzt = (bf16_t*)(ws + at.dzt);
-  bf16_t* xt = (bf16_t*)(ws + at.xt);
+  const int Np = round_up64(a.N);
+  const bool copy = (a.dx || a.dw) && (a.slope || !direct(a.dy, a.lddy, a.N));
+  const bf16_t* dz = copy ? (const bf16_t*)(ws + at.dz) : (const bf16_t*)a.dy;
+  const long lddz = copy ? Np : a.lddy;
   float* sums = (float*)(ws + at.sums);
+  const bool copy_x = a.dw && !direct(a.x, a.ldx, a.K);
+  const Rows x = copy_of(a.x, a.ldx, a.M, a.K, ws + at.x);
   hipError_t e = hipSuccess;
-  const Turn none{};
-  const Turn dz = copy || a.dw || a.db ? turn_of(a.dy, a.lddy, a.slope, a.M, a.N, a.dw ? dzt : nullptr, Mp, copy ? (bf16_t*)(ws + at.dz) : nullptr, Np, a.db ? sums : nullptr) : none;
-  const Turn x = a.dw ? turn_of(a.x, a.ldx, nullptr, a.M, a.K, xt, Mp, nullptr, 0, nullptr) : none;
-  if (dz.blocks) {
-    k_linear_turn<<<dz.blocks + x.blocks, 256, 0, s>>>(dz, x);
+  if (copy || a.db || copy_x) {
+    const int wide = direct(a.dy, a.lddy, a.N) && ((uintptr_t)a.slope & 15) == 0;
+    const Rows r{(const bf16_t*)a.dy, a.lddy, (const bf16_t*)a.slope, copy ? (bf16_t*)(ws + at.dz) : nullptr, Np, a.db ? sums : nullptr, a.M, a.N, wide, at.group};
+    const unsigned blocks = copy || a.db ? row_blocks(r) : 0;
+    k_linear_rows<<<blocks + (copy_x ? row_blocks(x) : 0), 256, 0, s>>>(r, x, blocks);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.db) {
-    k_linear_db_join<<<blocks64(a.N), 1024, 0, s>>>(sums, (a.M + 255) / 256, a.db, a.accumulate, a.N);
+    k_linear_db_join<<<blocks64(a.N), 1024, 0, s>>>(sums, at.groups, a.db, a.accumulate, a.N);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.dx) {
     Product p{};
-    p.A = copy ? (const bf16_t*)(ws + at.dz) : (const bf16_t*)a.dy; p.lda = copy ? Np : a.lddy;
+    p.A = dz; p.lda = lddz;
     p.B = (const bf16_t*)a.weights + (size_t)a.N * round_up64(a.K); p.ldb = Np;
     p.M = a.M; p.N = a.K; p.K = copy ? Np : a.N;
     p.y = (bf16_t*)a.dx; p.ldy = a.lddx;
-    e = product<OUT_Y>(p, (float*)(ws + at.slabs), s);
+    e = product<false>(p, (float*)(ws + at.slabs), s);
   }
   if (e == hipSuccess && a.dw) {
     Product p{};
-    p.A = xt; p.lda = Mp; p.B = dzt; p.ldb = Mp; p.M = a.K; p.N = a.N; p.K = Mp; p.sum = a.dw; p.accumulate = a.accumulate;
-    e = product<OUT_SUM>(p, (float*)(ws + at.slabs), s);
+    p.A = copy_x ? x.dst : (const bf16_t*)a.x; p.lda = copy_x ? x.ld : a.ldx;
+    p.widthA = copy_x ? x.ld : a.K;
+    p.B = dz; p.ldb = lddz; p.widthB = copy ? Np : a.N;
+    p.M = a.K; p.N = a.N; p.K = a.M; p.sum = a.dw; p.accumulate = a.accumulate;
+    e = product<true>(p, (float*)(ws + at.slabs), s);
   }
   return e;
 }
@@ -879,7 +889,7 @@ hipError_t launch_linear_pack(const float* w, bf16_t* packed, int K, int N, hipS
 
 size_t linear_workspace_bytes(int dt, int M, int K, int N) {
   if (dt != DT_BF16) return (size_t)M * N * sizeof(float);
-  const size_t f = align256((size_t)M * round_up64(K) * 2) + slab_bytes(M, N, round_up64(K)), b = BackwardSpace(M, K, N).bytes;
+  const size_t f = align256((size_t)M * round_up64(K) * 2) + slab_bytes(M, N, round_up64(K), false), b = BackwardSpace(M, K, N).bytes;
   return f > b ? f : b;
 }
 
