@@ -561,7 +561,7 @@ struct Rows {
   const bf16_t* slope;          // dense
   bf16_t* dst; int ld;
   float* sums;                  // [M / group][cols]
-  int M, cols, wide;            // wide: src and slope rows allow 16-byte loads
+  int M, cols;
   int group;                    // rows of a work-group, a multiple of 16
 };
 __global__ __launch_bounds__(256) void k_linear_rows(Rows first, Rows second, unsigned blocks) {       // blocks: of first
@@ -572,28 +572,28 @@ __global__ __launch_bounds__(256) void k_linear_rows(Rows first, Rows second, un
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = (int)(block / col_blocks), c0 = (int)(block % col_blocks) * 512, c = c0 + lane * 8;
   float sum[8] = {};
-  auto fetch = [&](const bf16_t* r, int m, uint32_t (&w)[4]) {
+  const int left = p.cols - c;
+  auto fetch = [&](const bf16_t* rows, long ld, int m0, uint32_t (&w)[4][4]) {      // four rows; behind the last one: that one
+    if (left >= 8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = 0;
-    if (m >= p.M || c >= p.cols) return;
-    if (p.wide) {               // cols is a multiple of 8
-      const uint4 q = *reinterpret_cast<const uint4*>(r + c);
-      w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+      for (int i = 0; i < 4; ++i) __builtin_memcpy(w[i], rows + (m0 + i < p.M ? m0 + i : p.M - 1) * ld + c, 16);      // any multiple of 2 bytes will do
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < p.cols) w[e >> 1] |= (uint32_t)r[c + e] << (16 * (e & 1));
+      for (int i = 0; i < 4; ++i) {
+        const bf16_t* r = rows + (m0 + i < p.M ? m0 + i : p.M - 1) * ld + c;
+        uint32_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? r[e] : 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[i][k] = v[2 * k] | v[2 * k + 1] << 16;
+      }
     }
   };
   const int each = p.group / 4, m0 = g * p.group + wave * each;
   for (int i0 = 0; i0 < each; i0 += 4) {
     uint32_t r[4][4], s[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const long m = m0 + i0 + i;
-      fetch(p.src + m * p.lds, (int)m, r[i]);
-      if (p.slope) fetch(p.slope + m * p.cols, (int)m, s[i]);
-    }
+    fetch(p.src, p.lds, m0 + i0, r);
+    if (p.slope) fetch(p.slope, p.cols, m0 + i0, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int m = m0 + i0 + i;
@@ -602,6 +602,7 @@ __global__ __launch_bounds__(256) void k_linear_rows(Rows first, Rows second, un
         if (p.slope)            // exact in fp32, then one rounding
           r[i][w] = pack_bf16x2(__uint_as_float(r[i][w] << 16) * __uint_as_float(s[i][w] << 16),
                                 __uint_as_float(r[i][w] & 0xffff0000u) * __uint_as_float(s[i][w] & 0xffff0000u));
+        if (m >= p.M) r[i][w] = 0;
         sum[2 * w] += __uint_as_float(r[i][w] << 16);
         sum[2 * w + 1] += __uint_as_float(r[i][w] & 0xffff0000u);
       }
@@ -766,7 +767,7 @@ unsigned row_blocks(const Rows& r) { return (unsigned)((r.M + r.group - 1) / r.g
 // a copy whose rows start on 16 bytes
 Rows copy_of(const void* x, long ldx, int M, int K, char* to) {
   const int Kp = round_up64(K);
-  return Rows{(const bf16_t*)x, ldx, nullptr, (bf16_t*)to, Kp, nullptr, M, K, 0, group_of(M, Kp)};
+  return Rows{(const bf16_t*)x, ldx, nullptr, (bf16_t*)to, Kp, nullptr, M, K, group_of(M, Kp)};
 }
 
 hipError_t forward_bf16(const LinearForward& a, char* ws, hipStream_t s) {
@@ -813,8 +814,7 @@ hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
   const Rows x = copy_of(a.x, a.ldx, a.M, a.K, ws + at.x);
   hipError_t e = hipSuccess;
   if (copy || a.db || copy_x) {
-    const int wide = direct(a.dy, a.lddy, a.N) && ((uintptr_t)a.slope & 15) == 0;
-    const Rows r{(const bf16_t*)a.dy, a.lddy, (const bf16_t*)a.slope, copy ? (bf16_t*)(ws + at.dz) : nullptr, Np, a.db ? sums : nullptr, a.M, a.N, wide, at.group};
+    const Rows r{(const bf16_t*)a.dy, a.lddy, (const bf16_t*)a.slope, copy ? (bf16_t*)(ws + at.dz) : nullptr, Np, a.db ? sums : nullptr, a.M, a.N, at.group};
     const unsigned blocks = copy || a.db ? row_blocks(r) : 0;
     k_linear_rows<<<blocks + (copy_x ? row_blocks(x) : 0), 256, 0, s>>>(r, x, blocks);
     e = hipGetLastError();
