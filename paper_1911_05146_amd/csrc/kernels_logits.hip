@@ -558,7 +558,7 @@ __device__ __forceinline__ float logit_of(const T* s, int label, int classes) {
 
 // rows that a wave or 256 threads hold: many of them on a CU at a time
 template <class T, int NT, int J, int PER>       // PER: rows per work-group
-__global__ __launch_bounds__(NT * PER) void k_logprob_forward(LogprobForward a) {
+__global__ __launch_bounds__(NT * PER, NT == 512 ? 4 : 1) void k_logprob_forward(LogprobForward a) {
   __shared__ GroupSpace<NT> space[PER];
   const int which = PER == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
   const Group<NT> g{space[which], (int)threadIdx.x % NT};
@@ -578,12 +578,14 @@ __global__ __launch_bounds__(1024) void k_logprob_rows(LogprobForward a) {
   typedef Held<T, 1024, J> H;
   __shared__ GroupSpace<1024> space;
   extern __shared__ __align__(16) uint4 room[];
-  const Group<1024> g{space, (int)threadIdx.x};
   int row = blockIdx.x;
   const T* s = (const T*)a.logits + row * a.ld;
-  H::template fetch<AHEAD>(s, a.classes, g.tid, room);
+  H::template fetch<AHEAD>(s, a.classes, (int)threadIdx.x, room);
   for (; row < a.rows; row += gridDim.x) {
     s = (const T*)a.logits + row * a.ld;
+    int t = (int)threadIdx.x;
+    asm("" : "+v"(t));                               // a row's own: else the compiler keeps what all rows have in common, indices above all
+    const Group<1024> g{space, t};
     H h;
     __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the thread's units are in LDS
     h.template load<AHEAD>(s, a.classes, g.tid, room);
@@ -1159,7 +1161,8 @@ hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hip
     if (a.rows <= SPREAD_ROWS) k_logprob_forward<T, 64, 4, 1><<<(unsigned)a.rows, 64, 0, s>>>(a);
     else k_logprob_forward<T, 64, 4, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
   } else if (c.units <= 256 * 8) k_logprob_forward<T, 256, 8, 1><<<(unsigned)a.rows, 256, 0, s>>>(a);
-  else if (c.units <= 1024 * 8) return launch_rows(k_logprob_rows<T, 8, 8>, 8, s, a);
+  else if (c.units <= 512 * 8) k_logprob_forward<T, 512, 8, 1><<<(unsigned)a.rows, 512, 0, s>>>(a);
+  else if (c.units <= 512 * 16) k_logprob_forward<T, 512, 16, 1><<<(unsigned)a.rows, 512, 0, s>>>(a);
   else return launch_rows(k_logprob_rows<T, 16, 8>, 8, s, a);
   return hipGetLastError();
 }
