@@ -327,15 +327,22 @@ struct Held {
   // unit u lies across an end of the row
   __device__ __forceinline__ void edge(const T* p, int u, uint32_t none) {
     uint32_t w[4] = {none, none, none, none};
-    if (u % NT == tid)
+    if (u % NT == tid) {
+      uint32_t x[E];              // none behind a condition, so that all are on their way together
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = u * E - shift + e, at = i < 0 ? 0 : i < len ? i : len - 1;
+        if constexpr (sizeof(T) == 4) x[e] = __float_as_uint(p[at]); else x[e] = p[at];
+      }
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const int i = u * E - shift + e;
         if (i >= 0 && i < len) {
-          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(p[i]);
-          else w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | (uint32_t)p[i] << 16 : (w[e >> 1] & 0xffff0000u) | p[i];
+          if constexpr (sizeof(T) == 4) w[e] = x[e];
+          else w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | x[e] << 16 : (w[e >> 1] & 0xffff0000u) | x[e];
         }
       }
+    }
 #pragma unroll
     for (int j = 0; j < J; ++j)
       if (u / NT == j && u % NT == tid) {
@@ -975,8 +982,48 @@ __global__ __launch_bounds__(NT * PER) void k_distill(Distill a) {
   if (g.tid < 64) l = read_list(a, s, row, g.tid);
   distill_row<HARD>(a, g, h, ans, l, row);
 }
-// Long rows, like k_logprob_rows; the units that LDS has no room for follow into their registers as the gradient leaves them.  Loss and entries are left to k_distill_entries, which finds the rows' sums in `records`: their double
-// arithmetic next to a row in registers costs more registers than there are.
+// Long rows: loss and entries are left to k_distill_entries, which finds the rows' sums in `records`: their double arithmetic next to a row in
+// registers costs more registers than there are.  What there is to know before the sums, and the gradient's factors from them:
+struct Before {
+  int label; bool has; float weight;
+  __device__ __forceinline__ Before(const Distill& a, int row, int tid, int& flags) {      // flags: in LDS, to be read behind a barrier
+    label = label_of(a.labels, row);
+    has = label >= 0 && label < a.classes;
+    weight = a.row_weight ? a.row_weight[row] : 1.f;
+    if (tid < 64) {
+      const int index = tid < a.top ? a.top_index[(long)row * a.top + tid] : -1;
+      const bool on = index >= 0 && a.top_logit[(long)row * a.top + tid] != -INF;
+      const bool some = __any(on), broken = __any(on && index >= a.classes);
+      if (tid == 0) flags = (int)some | (int)broken << 1;
+    }
+  }
+};
+struct Factors {
+  float soft, hard; bool zero;
+  template <int HARD>
+  static __device__ __forceinline__ Factors of(const Distill& a, const Before& b, const Soft& v, int flags) {
+    const bool some = flags & 1, empty = v.m == -INF;
+    const bool bad = v.m == INF || v.restt != v.restt || (HARD && v.rest1 != v.rest1) || (flags & 2) || (b.label != -1 && !b.has);
+    return Factors{bad ? quiet_nan() : some ? b.weight * (1.f - a.hard_weight) * a.temperature / (1.f + v.restt) : 0.f,
+                   bad ? quiet_nan() : HARD && b.has ? b.weight * a.hard_weight / (1.f + v.rest1) : 0.f, empty && !bad};
+  }
+};
+template <int HARD, class T, int NT, int J>
+__global__ __launch_bounds__(NT, 4) void k_distill_held(Distill a, Soft* records) {
+  __shared__ GroupSpace<NT> space;
+  const Group<NT> g{space, (int)threadIdx.x};
+  const float it = 1.f / a.temperature;
+  const int row = blockIdx.x;
+  const T* s = (const T*)a.logits + row * a.ld;
+  Held<T, NT, J> h;
+  h.load(s, a.classes, g.tid);
+  const Before b(a, row, g.tid, space.n);
+  const Soft v = soft_of<HARD>(g, h, it);
+  const Factors f = Factors::of<HARD>(a, b, v, space.n);
+  if (g.tid == 0) records[row] = v;
+  if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, f.zero, [](int) {});
+}
+// Longer ones, like k_logprob_rows; the units that LDS has no room for follow into their registers as the gradient leaves them.
 template <int HARD, class T, int J, int AHEAD>
 __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records) {
   typedef Held<T, 1024, J> H;
@@ -995,29 +1042,16 @@ __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records)
     s = (const T*)a.logits + row * a.ld;
     const bool more = row + (int)gridDim.x < a.rows;
     const T* next = s + gridDim.x * a.ld;
-    h.template load<AHEAD, AHEAD < J ? AHEAD : J>(s, a.classes, g.tid, room);
-    const int label = label_of(a.labels, row);
-    const bool has = label >= 0 && label < a.classes;
-    const float w = a.row_weight ? a.row_weight[row] : 1.f;
-    if (g.tid < 64) {
-      const int index = g.tid < a.top ? a.top_index[(long)row * a.top + g.tid] : -1;
-      const bool on = index >= 0 && a.top_logit[(long)row * a.top + g.tid] != -INF;
-      const bool some = __any(on), broken = __any(on && index >= a.classes);
-      if (g.tid == 0) space.n = (int)some | (int)broken << 1;
-    }
+    h.template load<AHEAD, AHEAD>(s, a.classes, g.tid, room);
+    const Before b(a, row, g.tid, space.n);
     __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): they are read
     if (more) H::template fetch<AHEAD>(next, a.classes, g.tid, room);
     const Soft v = soft_of<HARD>(g, h, it);
-    const bool some = space.n & 1, empty = v.m == -INF;
-    const bool bad = v.m == INF || v.restt != v.restt || (HARD && v.rest1 != v.rest1) || (space.n & 2) || (label != -1 && !has);
+    const Factors f = Factors::of<HARD>(a, b, v, space.n);
     if (g.tid == 0) records[row] = v;
     __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the next row's units are in LDS; before the stores, whose end nobody awaits
     auto after = [&](int j) { if (j >= AHEAD && more) h.load_unit(next, a.classes, g.tid, j, nullptr); };
-    if (a.dlogits) {
-      const float fs = bad ? quiet_nan() : some ? w * (1.f - a.hard_weight) * a.temperature / (1.f + v.restt) : 0.f;
-      const float fh = bad ? quiet_nan() : HARD && has ? w * a.hard_weight / (1.f + v.rest1) : 0.f;
-      write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, fs, fh, empty && !bad, after);
-    }
+    if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, f.zero, after);
     if (!a.dlogits || !h.used(J - 1)) {                // units that this row does not have, but the next may
 #pragma unroll
       for (int j = AHEAD; j < J; ++j)
@@ -1133,6 +1167,11 @@ RowCut row_cut(int dt, int rows, int classes, bool aligned) {
   return c;
 }
 
+// Whether an undivided row of a distillation leaves loss and entries to a second launch, for which the workspace holds the rows' sums.  A wave
+// that has a row to itself never does; 256 threads do where there are rows enough for the second launch not to count (4096 rows of 8200: 48
+// instead of 59 us; 300 of 5000: 16.8 instead of 12.1).
+bool by_records(int rows, int units) { return units > 256 * 8 || (units > 64 * 4 && rows > SPREAD_ROWS); }
+
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 bool aligned16(const void* p, long ld, size_t elem) { return ((uintptr_t)p & 15) == 0 && ((size_t)ld * elem & 15) == 0; }
 
@@ -1190,10 +1229,15 @@ hipError_t distill_as(int dt, const Distill& a, void* workspace, hipStream_t s) 
     constexpr int ANY = HARD ? HARD_EXP : HARD_NONE;
     if (a.rows <= SPREAD_ROWS) k_distill<ANY, T, 64, 4, 1><<<(unsigned)a.rows, 64, 0, s>>>(a);
     else k_distill<ANY, T, 64, 4, 4><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a);
-  } else if (c.units <= 256 * 8) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 256, 8, 1><<<(unsigned)a.rows, 256, 0, s>>>(a);
+  } else if (!by_records(a.rows, c.units)) k_distill<HARD ? HARD_EXP : HARD_NONE, T, 256, 8, 1><<<(unsigned)a.rows, 256, 0, s>>>(a);
   else {
     Soft* records = (Soft*)workspace;
-    const hipError_t e = c.units <= 1024 * 8 ? launch_rows(k_distill_rows<HARD, T, 8, 8>, 8, s, a, records) : launch_rows(k_distill_rows<HARD, T, 16, 8>, 8, s, a, records);
+    hipError_t e = hipSuccess;
+    if (c.units <= 256 * 8) k_distill_held<HARD, T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(a, records);
+    else if (c.units <= 512 * 8) k_distill_held<HARD, T, 512, 8><<<(unsigned)a.rows, 512, 0, s>>>(a, records);
+    else if (c.units <= 512 * 16) k_distill_held<HARD, T, 512, 16><<<(unsigned)a.rows, 512, 0, s>>>(a, records);
+    else e = launch_rows(k_distill_rows<HARD, T, 16, 8>, 8, s, a, records);
+    if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return e;
     k_distill_entries<T><<<(unsigned)((a.rows + 3) / 4), 256, 0, s>>>(a, records);
   }
@@ -1215,7 +1259,7 @@ size_t logits_workspace_bytes(int dt, int rows, int classes, int top) {
   const RowCut c = row_cut(dt, rows, classes, false);
   const size_t n = (size_t)rows * c.parts;
   if (c.parts > 1) return align256(n * sizeof(PartRecord)) + align256(n * top * sizeof(Key));
-  return c.units > 256 * 8 ? align256(n * sizeof(Soft)) : 0;
+  return by_records(rows, c.units) ? align256(n * sizeof(Soft)) : 0;
 }
 
 hipError_t launch_logprob_forward(int dt, const LogprobForward& a, void* workspace, hipStream_t stream) {

@@ -453,3 +453,91 @@ def test_lists_among_thousands_of_large_logits(env, mode, classes, period, part,
         check_forward(torch, s, labels, n, ops[mode].logprob_forward(s, labels, n))
     views = torch.cat([torch.zeros(4, 3, device="cuda", dtype=s.dtype), s], 1)[:, 3:]
     check_forward(torch, views, labels, top, ops[mode].logprob_forward(views, labels, top))
+
+
+# As many rows as there are when none is divided among work-groups, at lengths on both sides of every kernel's
+MANY = [(1100, 2052), (1030, 9001), (200, 20001), (140, 32768), (300, 50001), (140, 65536), (140, 65537), (260, 131072)]
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s)))
+def test_many_long_rows(env, mode, shape):
+    hpf, torch, ops = env
+    print(f"\n[case] many rows {shape} {mode}", flush=True)
+    s, labels, g = make(torch, mode, *shape)
+    for top in (0, 64):
+        r = ops[mode].logprob_forward(s, labels, top)
+        check_forward(torch, s, labels, top, r)
+        again = ops[mode].logprob_forward(s, labels, top)
+        assert all(p is None or torch.equal(p, q) for p, q in zip(r, again)), "same inputs, other bits"
+    index, logit = teacher(torch, s, 20, g)
+    weight = torch.randn(shape[0], device="cuda", generator=g)
+    for T, hw in ((1.0, 0.25), (2.0, 0.5), (4.0, 0.1), (0.7, 0.9), (3.0, 0.0)):
+        loss, ds = ops[mode].distill(s, index, logit, labels, temperature=T, hard_weight=hw, row_weight=weight)
+        check_distill(torch, mode, s, index, logit, labels, T, hw, weight, loss, ds)
+        alone, none = ops[mode].distill(s, index, logit, labels, temperature=T, hard_weight=hw, row_weight=weight, gradient=False)
+        assert none is None and torch.equal(loss, alone)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1030, 9001), (200, 20001), (300, 50001), (260, 131000)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("left,right", [(1, 0), (3, 4)])
+def test_views_of_many_long_rows(env, mode, shape, left, right):
+    test_views_give_what_dense_rows_give(env, mode, shape, left, right)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("copies,classes", [(110, 2100), (20, 20000), (20, 40000), (30, 50000), (30, 131000)])
+def test_masked_and_broken_rows_among_many(env, mode, copies, classes):
+    """Ten special rows over and over: each copy like the first one, bit for bit, and like the ten alone, which other kernels take: to twice
+    the bound that holds for either, with sum p |t| <= 30 and an entropy of at most log(131000) < 12."""
+    hpf, torch, ops = env
+    lowest = torch.finfo(torch.bfloat16 if mode == "bf16" else torch.float32).min
+    s, _, g = make(torch, mode, 10, classes, seed=3)
+    labels = torch.tensor([0, 1, 2, 3, 4, -1, classes - 1, classes, -7, 2], device="cuda", dtype=torch.int32)
+    s[0] = s[5] = -INF
+    s[1, :] = -INF
+    s[1, 1] = 2.0
+    s[2, :] = lowest
+    s[2, 2], s[2, 3] = 1.0, 1.0
+    s[3, classes // 2] = float("nan")
+    s[4, classes - 2] = INF
+    s[6] = lowest
+    s[9, :] = -INF
+    s[9, 0], s[9, 3] = 0.0, 0.0
+    index = torch.tensor([[2, 3, -1]] * 7 + [[5, classes, 1], [1, 1, 0], [0, 3, 7]], device="cuda", dtype=torch.int32)
+    logit = torch.tensor([[0.0, 1.0, 2.0]] * 10, device="cuda")
+    few = ops[mode].logprob_forward(s, labels, 30)
+    many = ops[mode].logprob_forward(s.repeat(copies, 1), labels.repeat(copies), 30)
+    few_d = ops[mode].distill(s, index, logit, labels, temperature=2.0, hard_weight=0.5)
+    many_d = ops[mode].distill(s.repeat(copies, 1), index.repeat(copies, 1), logit.repeat(copies, 1), labels.repeat(copies), temperature=2.0, hard_weight=0.5)
+    rel = 2.0 ** -23 * 64 + (classes / 64 + 64) * 2.0 ** -24
+    for name, a, b in [(n, getattr(few, n), getattr(many, n)) for n in few._fields] + [("loss", few_d[0], many_d[0]), ("dlogits", few_d[1], many_d[1])]:
+        b = b.view(copies, *a.shape)
+        same = (b == b[:1]) | (b.isnan() & b[:1].isnan())
+        assert bool(same.all()), f"{name}: copies of a row differ"
+        if a.dtype == torch.int32:
+            assert torch.equal(a, b[0]), name
+            continue
+        a = a.double()
+        size = 2.0 ** -23 * torch.where(a.isinf() | a.isnan(), 0.0, a.abs())
+        tol = 2 * (size + rel * (25 if name == "entropy" else 4 if name == "loss" else 1))
+        near(b[0], a, tol if name != "dlogits" else tol + 2 * HALF[mode] * a.abs(), name)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("classes,period,part", [(9000, 1024, 192), (20000, 2048, 384), (50000, 4096, 128), (131072, 8192, 256)])
+def test_lists_among_thousands_of_large_logits_of_many_rows(env, mode, classes, period, part):
+    hpf, torch, ops = env
+    g = torch.Generator(device="cuda").manual_seed(classes)
+    c = torch.arange(classes, device="cuda")
+    s = torch.randn(260, classes, device="cuda", generator=g)
+    large = (c % period) < part
+    s[:130] += 30.0 * large
+    s[65:195] = s[65:195].round()
+    s[195:230] = torch.where(large, 7.0, 6.0)
+    s[230:] = 1.0
+    s = s.to(torch.bfloat16 if mode == "bf16" else torch.float32)
+    labels = torch.randint(0, classes, (260,), device="cuda", generator=g).int()
+    for top in (5, 64):
+        check_forward(torch, s, labels, top, ops[mode].logprob_forward(s, labels, top))
