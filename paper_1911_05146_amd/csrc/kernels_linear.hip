@@ -159,20 +159,20 @@ struct Product {
 
 __device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};   // where lanes beyond the end of a row read
 
-// Phi(z) and the normal density by one exponential: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26
-// (absolute error of erfc 1.5e-7, a hundredth of a bf16 step at 1)
-__device__ __forceinline__ void normal(float z, float& below, float& density) {
-  const float x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f)), e = __expf(-x * x);
-  const float q = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+// Phi(z) and sqrt(2 pi) times the normal density by one exponential: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, with
+// x = |z| / sqrt 2 and the half of erfc in the coefficients (absolute error of erfc 1.5e-7, a hundredth of a bf16 step at 1)
+__device__ __forceinline__ void normal(float z, float& below, float& e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  e = __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504f));
+  const float q = e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f);
   below = z < 0.f ? q : 1.f - q;
-  density = 0.39894228f * e;
 }
 __device__ __forceinline__ void activate_fast(int act, float z, float& y, float& slope) {
   if (act == ACT_GELU) {
-    float below, density;
-    normal(z, below, density);
+    float below, e;
+    normal(z, below, e);
     y = z * below;
-    slope = fmaf(z, density, below);
+    slope = fmaf(z * 0.39894228f, e, below);
   } else if (act == ACT_SILU) {
     const float q = __builtin_amdgcn_rcpf(1.f + __expf(-z));
     y = z * q;

@@ -896,8 +896,8 @@ struct Answer {
     logl = has && hard ? (double)mine - (double)v.m - log1p((double)v.rest1) : 0.0;
     ws = some ? w * (1.0 - hw) * a.temperature : 0.0;
     wh = has ? w * hw : 0.0;
-    fs = bad ? quiet_nan() : (float)(ws / (1.0 + v.restt));
-    fh = bad ? quiet_nan() : hard ? (float)(wh / (1.0 + v.rest1)) : 0.f;
+    fs = bad ? quiet_nan() : empty ? 0.f : (float)(ws / (1.0 + v.restt));
+    fh = bad ? quiet_nan() : hard && !empty ? (float)(wh / (1.0 + v.rest1)) : 0.f;
   }
   __device__ __forceinline__ void write_loss(const List& l) const {
     const double hw = (double)a.hard_weight;
@@ -932,14 +932,14 @@ struct Answer {
 
 // gradient of the `len` held elements to d
 template <int HARD, class T, int NT, int J, class G>
-__device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, bool zero, G after) {
+__device__ __forceinline__ void write_gradient(Held<T, NT, J>& h, T* d, float m, float it, float fs, float fh, G after) {
   const Exponents x(m, it);
   h.renew();
   h.store(d, [&](float s, int, int) {
     const float e = x.soft(s);
     float y = fs * e;
     if (HARD) y = fmaf(fh, x.hard<HARD>(s, e), y);
-    return zero ? 0.f : y;
+    return y;
   }, after);
 }
 
@@ -963,7 +963,7 @@ __device__ __forceinline__ void distill_row(const Distill& a, const Group<NT>& g
   T* d = (T*)a.dlogits + row * a.ldd;
   typename Answer<T>::Entries entries{-1, -1, 0.f, 0.f};
   if (g.tid < 64) entries = ans.entries(l, g.tid);
-  write_gradient<HARD>(h, d, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad, [](int) {});
+  write_gradient<HARD>(h, d, v.m, it, ans.fs, ans.fh, [](int) {});
   if (NT > 64) __syncthreads(); else __builtin_amdgcn_s_waitcnt(0x0f70);   // the stores above are done before the entries replace some of them
   if (g.tid < 64) Answer<T>::write(entries, d, 0, a.classes);
 }
@@ -999,13 +999,13 @@ struct Before {
   }
 };
 struct Factors {
-  float soft, hard; bool zero;
+  float soft, hard;
   template <int HARD>
   static __device__ __forceinline__ Factors of(const Distill& a, const Before& b, const Soft& v, int flags) {
-    const bool some = flags & 1, empty = v.m == -INF;
+    const bool some = (flags & 1) && v.m != -INF, hot = b.has && v.m != -INF;      // nothing for a row that is masked whole
     const bool bad = v.m == INF || v.restt != v.restt || (HARD && v.rest1 != v.rest1) || (flags & 2) || (b.label != -1 && !b.has);
     return Factors{bad ? quiet_nan() : some ? b.weight * (1.f - a.hard_weight) * a.temperature / (1.f + v.restt) : 0.f,
-                   bad ? quiet_nan() : HARD && b.has ? b.weight * a.hard_weight / (1.f + v.rest1) : 0.f, empty && !bad};
+                   bad ? quiet_nan() : HARD && hot ? b.weight * a.hard_weight / (1.f + v.rest1) : 0.f};
   }
 };
 template <int HARD, class T, int NT, int J>
@@ -1021,7 +1021,7 @@ __global__ __launch_bounds__(NT, 4) void k_distill_held(Distill a, Soft* records
   const Soft v = soft_of<HARD>(g, h, it);
   const Factors f = Factors::of<HARD>(a, b, v, space.n);
   if (g.tid == 0) records[row] = v;
-  if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, f.zero, [](int) {});
+  if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, [](int) {});
 }
 // Longer ones, like k_logprob_rows; the units that LDS has no room for follow into their registers as the gradient leaves them.
 template <int HARD, class T, int J, int AHEAD>
@@ -1051,7 +1051,7 @@ __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records)
     if (g.tid == 0) records[row] = v;
     __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): the next row's units are in LDS; before the stores, whose end nobody awaits
     auto after = [&](int j) { if (j >= AHEAD && more) h.load_unit(next, a.classes, g.tid, j, nullptr); };
-    if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, f.zero, after);
+    if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, after);
     if (!a.dlogits || !h.used(J - 1)) {                // units that this row does not have, but the next may
 #pragma unroll
       for (int j = AHEAD; j < J; ++j)
@@ -1130,7 +1130,7 @@ __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long
     step = c_end - c0 < room ? c_end - c0 : room;
     H h;
     h.load(s + c0, (int)step, tid);
-    write_gradient<HARD>(h, d + c0, v.m, it, ans.fs, ans.fh, ans.empty && !ans.bad, [](int) {});
+    write_gradient<HARD>(h, d + c0, v.m, it, ans.fs, ans.fh, [](int) {});
   }
   __syncthreads();
   if (tid < 64) Answer<T>::write(ans.entries(l, tid), d, c_begin, c_end);
