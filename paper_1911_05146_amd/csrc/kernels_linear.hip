@@ -56,7 +56,7 @@ struct Epilogue {
 
 // fp32 (check mode): C tile of 32 x 32 by eight waves, four of 16 x 16 for each half of the 64 steps that are staged at a time; the halves are
 // joined at the end.  v_mfma_f64_16x16x4_f64 takes 64 cycles, so small tiles, which give every CU one, cost nothing: 333 x 1000 x 517 has 187 of
-// them (64 x 64 ones with four waves: 54, and 144 us instead of TILE_F32 us).  Any sizes and strides.
+// them (64 x 64 ones with four waves: 54, and 144 us instead of 26).  Any sizes and strides.
 __global__ __launch_bounds__(512) void k_linear_tile_f32(Operand A, Operand B, Epilogue e, int M, int N, int K) {
   constexpr int KS = 64, LS = KS + 4;
   __shared__ __align__(16) float sA[32 * LS], sB[32 * LS];
@@ -185,8 +185,8 @@ __device__ __forceinline__ void activate_fast(int act, float z, float& y, float&
 __host__ __device__ constexpr int slab_row(int n) { return (n + 7) & ~7; }       // rows of partial sums start on 32 bytes
 
 // Eight consecutive results of a row, n a multiple of 8.  The bias and, where rows allow 16-byte loads, the residual are asked for ahead of the
-// sums they join: one at a time they cost a trip to memory for every 16 rows of a tile (residual, bias, gelu and slope at 8192 x 4096 x 4096:
-// 65 us on top of the product, now 43).
+// sums they join: one at a time they cost a trip to memory for every 16 rows of a tile.  Residual, bias, gelu and slope at 8192 x 4096 x 4096 take
+// 54 us on top of the product's 200 (76 so), 32 of them what their bytes take.
 struct Ahead { float bias[8]; };
 __device__ __forceinline__ bool wide_rows(const bf16_t* p, long ld) { return (ld & 7) == 0 && ((uintptr_t)p & 15) == 0; }
 template <int OUT>
@@ -310,8 +310,9 @@ __device__ __forceinline__ void stage_barrier() {
 //
 // ROWS: a stage is 64 rows of BM and of BN columns, and ds_read_b64_tr_b16 turns them on the way into the registers: from four rows' 4 x 16
 // elements every lane of 16 gets a column's four.  The 32-byte pieces of a row are stored in the order piece ^ f(row), with f over the 16 rows
-// of a read such that no more than two of them share banks, and two trips are what 512 bytes take anyway.  Turned copies of both operands
-// instead cost a pass over each: 75 us at 8192 x 4096 x 4096, of which 33 remain for dz = dy * slope.
+// of a read such that no more than two of them share banks, and two trips are what 512 bytes take anyway.  dw of 4096 x 4096 from 8192 rows,
+// within a backward call: 240 us (dx: 249).  Turned copies of both operands instead were a pass over each before it, 85 us, of which 44 remain
+// for dz = dy * slope.
 template <int BM, int BN, int WM, int WN, int STAGES, int OUT, bool ROWS>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigned tile_rows, unsigned tile_cols, int steps_per_split) {
   constexpr int NT = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * 64;
@@ -692,8 +693,13 @@ unsigned grid_for(size_t n, size_t per, size_t cap) {
 }
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-// How a bf16 product is cut: 256 x 256 tiles where they fill the chip, 128 x 128 ones where those do; else 64 x 64 ones, two work-groups of four
-// stages per CU, with the contraction split until there is a work-group per CU; up to 16 rows by k_linear_few.
+// How a bf16 product is cut (M x K x N, us):
+// - 256 x 256 tiles where there are 160 (2560 x 4096 x 4096, 160 tiles: 84, with 128 x 128 ones 97; 2048 x 4096 x 4096, 128 tiles: 78 and 67);
+// - 128 x 128 ones where there are 256 (2048 x 4096 x 2048, 256 tiles: 52, with 64 x 64 ones 61; 1536 x 4096 x 1536, 144 tiles: 42 and 37);
+// - 64 x 64 ones, two work-groups of four stages per CU, with the contraction split until there is a work-group per CU;
+// - k_linear_few for up to 16 rows of small weights, where a launch less counts most.  It reads K N weights once and x again for every 16
+//   columns, K N M / 16, and takes up to 1.25 * 2^25 of both (4096 x 4096: 13.2 to 11.9 for 1 to 16 rows, with 64 x 64 tiles 14.5 to 13.9;
+//   4096 x 8192: 13.0 and 14.6 for one row, 17.4 and 15.1 for 16; 4096 x 32000: 40 and 37, 58 and 37).
 enum : int { CUT_LARGE, CUT_TILES, CUT_SPLIT, CUT_FEW };
 struct Cut {
   int kind, splits, steps;      // steps (of 64, CUT_FEW: 32) per share
@@ -702,7 +708,8 @@ struct Cut {
 Cut cut_of(int M, int N, int K, bool rows) {      // rows: of a ROWS product
   auto tiles = [&](int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   Cut c;
-  c.kind = M <= 16 && !rows ? CUT_FEW : tiles(256, 256) >= 192 ? CUT_LARGE : tiles(128, 128) >= 256 ? CUT_TILES : CUT_SPLIT;
+  const bool few = M <= 16 && !rows && (long)K * N * (16 + M) <= 20l << 25;
+  c.kind = few ? CUT_FEW : tiles(256, 256) >= 160 ? CUT_LARGE : tiles(128, 128) >= 256 ? CUT_TILES : CUT_SPLIT;
   const int bm = c.kind == CUT_FEW ? 16 : c.kind == CUT_LARGE ? 256 : c.kind == CUT_TILES ? 128 : 64, bn = bm;
   c.rows = (unsigned)((M + bm - 1) / bm);
   c.cols = (unsigned)((N + bn - 1) / bn);
@@ -761,7 +768,8 @@ hipError_t product(const Product& p, float* slabs, hipStream_t s) {
 // Rows that the tiles read where they are: 16-byte units, and 256 rows within 32-bit offsets
 bool direct(const void* p, long ld, int K) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (K & 7) == 0 && ld <= 1 << 22; }
 
-// Rows in a work-group of k_linear_rows: 64, or 16 while that gives no CU two work-groups (1021 x 1000: 11.6 with 64, ROWS16 us with 16)
+// Rows in a work-group of k_linear_rows: 64, or 16 while that gives no CU two work-groups (gradients of 1021 x 2049 x 1000: 47.8 us
+// with 64, 43.6 with 16; of 8192 x 4096 x 4096, where 64 it is, no difference, but a quarter of the sums)
 int group_of(int M, int width) { return (long)((M + 63) / 64) * ((width + 511) / 512) >= 512 ? 64 : 16; }
 unsigned row_blocks(const Rows& r) { return (unsigned)((r.M + r.group - 1) / r.group) * (unsigned)((r.ld + 511) / 512); }
 // a copy whose rows start on 16 bytes
