@@ -406,7 +406,8 @@ hpf_status hpf_op_bn_relu_forward_noalloc(hpf_dtype dtype, const void* x, const 
  * without an element, sums over no rows are zero).  Every call only enqueues work, keeps nothing behind, and gives the
  * same bits for the same inputs; it may be captured into a graph.  `workspace` (256-byte aligned, may be NULL where its
  * size is 0) holds nothing from one call to the next; calls that can overlap in time need workspaces of their own.
- * No output may overlap another tensor of the call except where a call says so.
+ * No output may overlap another tensor of the call except where a call says so (columns of one wider matrix, side by side, do not
+ * overlap).
  *
  * Products.  dtype is the type of x, y, residual, slope, dy and dx; weights, bias and their gradients are fp32 masters
  * (w [K][N]).  HPF_BF16: the products take bf16 copies of the weights, which hpf_op_linear_pack lays out once after every

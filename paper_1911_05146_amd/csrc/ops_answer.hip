@@ -16,11 +16,22 @@ bool type_of(hpf_dtype dtype, int& dt) {
 bool rows_ok(int64_t ld, int32_t cols) { return ld >= cols && ld <= (int64_t)1 << 40; }
 size_t elem(int dt) { return dt == DT_BF16 ? 2 : 4; }
 bool element_aligned(const void* p, int dt) { return (uintptr_t)p % elem(dt) == 0; }
-// bytes that a [rows, cols] matrix with row stride ld spans
-size_t span(int dt, int64_t rows, int64_t cols, int64_t ld) { return rows ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem(dt) : 0; }
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return a && b && x < y + nb && y < x + na;
+}
+// a [rows, cols] matrix with row stride ld, elements of e bytes; none without an address
+struct Matrix {
+  const void* p; int64_t rows, cols, ld; size_t e;
+  size_t span() const { return p && rows ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * e : 0; }
+};
+// Columns of one wider matrix, side by side, do not overlap.
+bool overlap(const Matrix& a, const Matrix& b) {
+  if (!a.span() || !b.span() || !overlap(a.p, a.span(), b.p, b.span())) return false;
+  const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p), e = (int64_t)a.e;
+  if (a.ld != b.ld || !a.ld || a.e != b.e || d % e) return true;
+  const int64_t at = ((d / e) % a.ld + a.ld) % a.ld;      // b's first column, counted from a's
+  return at < a.cols || at + b.cols > a.ld;
 }
 hpf_status launched(hipError_t e) { return e == hipSuccess ? HPF_OK : fail(HPF_EDEVICE, "launch failed: %s", hipGetErrorString(e)); }
 
@@ -81,10 +92,11 @@ hpf_status hpf_op_linear_forward(hpf_dtype dtype, const void* x, int64_t ldx, co
   if (!element_aligned(x, dt) || !element_aligned(y, dt) || !element_aligned(residual, dt) || !element_aligned(slope, dt))
     return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
-  const size_t ny = span(dt, M, N, ldy), nx = span(dt, M, K, ldx), ns = span(dt, M, N, N);
-  const size_t nw = dt == DT_BF16 ? hpf_op_linear_packed_bytes(K, N) : (size_t)K * N * 4;
-  if (overlap(x, nx, y, ny) || overlap(x, nx, slope, ns) || overlap(y, ny, slope, ns) || overlap(weights, nw, y, ny) || overlap(weights, nw, slope, ns) ||
-      (residual && (overlap(residual, span(dt, M, N, ldr), slope, ns) || (overlap(residual, span(dt, M, N, ldr), y, ny) && (residual != y || ldr != ldy)))))
+  const size_t e = elem(dt);
+  const Matrix in{x, M, K, ldx, e}, out{y, M, N, ldy, e}, kept{slope, M, N, N, e}, added{residual, M, N, ldr, e};
+  const Matrix w{weights, 1, dt == DT_BF16 ? (int64_t)hpf_op_linear_packed_bytes(K, N) : (int64_t)K * N * 4, 0, 1};
+  if (overlap(in, out) || overlap(in, kept) || overlap(out, kept) || overlap(w, out) || overlap(w, kept) || overlap(added, kept) ||
+      (overlap(added, out) && (residual != y || ldr != ldy)))
     return fail(HPF_EINVAL, "an output overlaps another tensor (only residual and y may be the same)");
   st = workspace_ok(workspace, workspace_bytes, linear_workspace_bytes(dt, M, K, N));
   if (st != HPF_OK) return st;
@@ -111,14 +123,15 @@ hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy,
   if (!element_aligned(dy, dt) || !element_aligned(x, dt) || !element_aligned(dx, dt) || !element_aligned(slope, dt))
     return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (dx && dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
-  const size_t ndy = span(dt, M, N, lddy), nx = dw ? span(dt, M, K, ldx) : 0, ns = slope ? span(dt, M, N, N) : 0, ndx = dx ? span(dt, M, K, lddx) : 0;
-  const size_t nw = !dx ? 0 : dt == DT_BF16 ? hpf_op_linear_packed_bytes(K, N) : (size_t)K * N * 4;
-  const struct { const void* p; size_t n; } in[] = {{dy, ndy}, {x, nx}, {slope, ns}, {weights, nw}}, out[] = {{dx, ndx}, {dw, dw ? (size_t)K * N * 4 : 0}, {db, db ? (size_t)N * 4 : 0}};
+  const size_t e = elem(dt);
+  const Matrix in[] = {{dy, M, N, lddy, e}, {dw ? x : nullptr, M, K, ldx, e}, {slope, M, N, N, e},
+                       {dx ? weights : nullptr, 1, dt == DT_BF16 ? (int64_t)hpf_op_linear_packed_bytes(K, N) : (int64_t)K * N * 4, 0, 1}};
+  const Matrix out[] = {{dx, M, K, lddx, e}, {dw, 1, (int64_t)K * N, 0, 4}, {db, 1, N, 0, 4}};
   for (int i = 0; i < 3; ++i) {
-    for (const auto& q : in)
-      if (out[i].n && q.n && overlap(out[i].p, out[i].n, q.p, q.n)) return fail(HPF_EINVAL, "an output overlaps an input");
+    for (const Matrix& q : in)
+      if (overlap(out[i], q)) return fail(HPF_EINVAL, "an output overlaps an input");
     for (int j = i + 1; j < 3; ++j)
-      if (out[i].n && out[j].n && overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(HPF_EINVAL, "two outputs overlap");
+      if (overlap(out[i], out[j])) return fail(HPF_EINVAL, "two outputs overlap");
   }
   st = workspace_ok(workspace, workspace_bytes, linear_workspace_bytes(dt, M, K, N));
   if (st != HPF_OK) return st;
@@ -173,7 +186,7 @@ hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t 
   if (grad_entropy && !entropy) return fail(HPF_EINVAL, "entropy is required with grad_entropy");
   if (!rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
   if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
-  if (overlap(logits, span(dt, rows, classes, ld), dlogits, span(dt, rows, classes, ldd)) && (logits != dlogits || ld != ldd))
+  if (overlap(Matrix{logits, rows, classes, ld, elem(dt)}, Matrix{dlogits, rows, classes, ldd, elem(dt)}) && (logits != dlogits || ld != ldd))
     return fail(HPF_EINVAL, "dlogits overlap the logits (they may be the same tensor)");
   const LogprobBackward a{logits, ld, labels, stats, grad_logprob, entropy, grad_entropy, dlogits, ldd, rows, classes};
   return launched(launch_logprob_backward(dt, a, (hipStream_t)hip_stream));
@@ -194,7 +207,7 @@ hpf_status hpf_op_distill(hpf_dtype dtype, const void* logits, int64_t ld, const
   if (hard_weight > 0.f && !labels) return fail(HPF_EINVAL, "labels are required with hard_weight > 0");
   if (dlogits && !rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
   if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
-  if (overlap(logits, span(dt, rows, classes, ld), dlogits, span(dt, rows, classes, ldd))) return fail(HPF_EINVAL, "dlogits overlap the logits");
+  if (overlap(Matrix{logits, rows, classes, ld, elem(dt)}, Matrix{dlogits, rows, classes, ldd, elem(dt)})) return fail(HPF_EINVAL, "dlogits overlap the logits");
   st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
   if (st != HPF_OK) return st;
   const Distill a{logits, ld, top_index, top_logit, labels, row_weight, loss, dlogits, ldd, temperature, hard_weight, top, rows, classes};

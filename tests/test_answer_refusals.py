@@ -163,3 +163,15 @@ def test_tensor_checks_of_the_wrapper(hpf):
         o.logprob_forward(x.float())
     with pytest.raises(ValueError, match="w:"):
         o.linear_weights(torch.zeros(4, 4))
+
+
+def test_columns_that_overlap(hpf):
+    """Matrices of one row stride: side by side they do not overlap; a shared column, or one that wraps into the next row, does."""
+    def f(y, **kw):
+        refused(hpf, hpf.HPF_EINVAL, "overlaps", lambda: forward(hpf, y=y, ldx=40, ldy=40, **kw))
+    for at in (0, 15, -7, 40, 2 * 40 + 15, -40 + 39, 33, 33 + 40):          # x: columns 0 to 15 of 40; y: 8 columns from `at`
+        f(A + 2 * at)
+    f(A + 2 * 17, r=A + 2 * 20, ldr=40)                             # residual within y
+    # no overlap: what is refused next is the workspace
+    for at in (16, 32, 20 + 40):
+        refused(hpf, hpf.HPF_ENOMEM, "workspace", lambda: forward(hpf, y=A + 2 * at, ldx=40, ldy=40, n=1))

@@ -315,3 +315,69 @@ def test_new_weights_in_place(env):
         assert torch.equal(ops[mode].linear_forward(d["x"], weights), ops[mode].linear_forward(d["x"], ops[mode].linear_weights(d2["w"])))
         with pytest.raises(ValueError):
             ops[mode].linear_weights(d["w"][:, :69].contiguous(), out=weights)
+
+
+@pytest.mark.parametrize("shape", [(4100, 640, 2600), (4097, 40, 2570), (4096, 128, 2560), (4096, 192, 2568), (700, 2600, 4104), (705, 2605, 4099), (40, 2600, 4104),
+                                   (130, 2560, 4096), (192, 2568, 4096), (2050, 40, 2050), (2048, 130, 2056)], ids=lambda s: "x".join(map(str, s)))
+def test_large_tiles_and_short_sums(env, shape):
+    """Forward or dw on the largest tiles, with one, two, three and more steps of the contraction, whole and ending within one."""
+    test_forward_every_activation(env, "bf16", shape)
+    test_backward(env, "bf16", shape)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 4096, 8200), (4, 1024, 17000), (16, 1000, 20011), (16, 600, 16384), (2, 9000, 4096), (16, 20000, 520), (1, 3, 70001)])
+def test_few_rows_of_wide_weights(env, M, K, N):
+    test_forward_every_activation(env, "bf16", (M, K, N))
+    test_backward(env, "bf16", (M, K, N))
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+def test_row_strides_beyond_a_tiles_offsets(env, mode):
+    """256 rows, 2^22 + 8 elements apart, are more than 32 bits of bytes from end to end."""
+    hpf, torch, ops = env
+    M, K, N, ld = 260, 24, 40, (1 << 22) + 8
+    d = make(torch, mode, M, K, N, seed=5)
+    weights = ops[mode].linear_weights(d["w"])
+    wide = torch.empty(M, ld, device="cuda", dtype=tdtype(torch, mode))
+    x, dy, out = wide[:, :K], wide[:, K:K + N], wide[:, 128:128 + N]
+    x.copy_(d["x"])
+    dy.copy_(d["dy"])
+    y = ops[mode].linear_forward(d["x"], weights, d["bias"], d["dy"], "relu")
+    assert torch.equal(y, ops[mode].linear_forward(x, weights, d["bias"], dy, "relu", out=out))
+    a, b = ops[mode].linear_backward(d["dy"], d["x"], weights), ops[mode].linear_backward(dy, x, weights)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+def test_columns_of_one_matrix(env, mode):
+    """Input, residual and output side by side in one buffer do not overlap; nothing else in it changes."""
+    hpf, torch, ops = env
+    M, K, N = 70, 33, 20
+    d = make(torch, mode, M, K, N, seed=6)
+    weights = ops[mode].linear_weights(d["w"])
+    wide = torch.full((M, 101), 7.0, device="cuda", dtype=tdtype(torch, mode))
+    x, residual, out = wide[:, 1:1 + K], wide[:, 1 + K:1 + K + N], wide[:, 60:60 + N]
+    x.copy_(d["x"])
+    residual.copy_(d["residual"])
+    before = wide.clone()
+    y = ops[mode].linear_forward(d["x"], weights, None, d["residual"], "silu")
+    assert torch.equal(y, ops[mode].linear_forward(x, weights, None, residual, "silu", out=out))
+    before[:, 60:60 + N] = y
+    assert torch.equal(wide, before)
+    for cols in (slice(K, K + N), slice(0, N), slice(1 + K - N, 1 + K)):       # these share a column with x
+        with pytest.raises(hpf.HpfError):
+            ops[mode].linear_forward(x, weights, out=wide[:, cols])
+    logits, d_wide = wide[:, :40], wide[:, 40:80]
+    labels = torch.randint(0, 40, (M,), device="cuda", dtype=torch.int32)
+    logits.normal_()
+    r = ops[mode].logprob_forward(logits, labels)
+    one = torch.ones(M, device="cuda")
+    want = ops[mode].logprob_backward(logits.contiguous(), labels, r.stats, one)
+    assert torch.equal(want, ops[mode].logprob_backward(logits, labels, r.stats, one, out=d_wide))
+    with pytest.raises(hpf.HpfError):
+        ops[mode].logprob_backward(logits, labels, r.stats, one, out=wide[:, 39:79])
+
+
+@pytest.mark.parametrize("shape", [(4100, 264, 2600), (300, 2560, 4104), (16, 1000, 30000)], ids=lambda s: "x".join(map(str, s)))
+def test_streams_and_graphs_on_the_largest_tiles(env, shape):
+    test_streams_and_graphs(env, shape)

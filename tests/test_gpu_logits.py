@@ -541,3 +541,8 @@ def test_lists_among_thousands_of_large_logits_of_many_rows(env, mode, classes, 
     labels = torch.randint(0, classes, (260,), device="cuda", generator=g).int()
     for top in (5, 64):
         check_forward(torch, s, labels, top, ops[mode].logprob_forward(s, labels, top))
+
+
+@pytest.mark.parametrize("shape", [(1030, 9001), (200, 20001), (140, 65536), (300, 70001)], ids=lambda s: "x".join(map(str, s)))
+def test_streams_and_graphs_of_many_rows(env, shape):
+    test_streams_and_graphs(env, shape)
