@@ -56,7 +56,7 @@ struct Epilogue {
 
 // fp32 (check mode): C tile of 32 x 32 by eight waves, four of 16 x 16 for each half of the 64 steps that are staged at a time; the halves are
 // joined at the end.  v_mfma_f64_16x16x4_f64 takes 64 cycles, so small tiles, which give every CU one, cost nothing: 333 x 1000 x 517 has 187 of
-// them (64 x 64 ones with four waves: 54, and 144 us instead of 26).  Any sizes and strides.
+// them (64 x 64 ones with four waves: 54, and 144 us instead of 26, a fifth of the rate of a large product in double).  Any sizes and strides.
 __global__ __launch_bounds__(512) void k_linear_tile_f32(Operand A, Operand B, Epilogue e, int M, int N, int K) {
   constexpr int KS = 64, LS = KS + 4;
   __shared__ __align__(16) float sA[32 * LS], sB[32 * LS];
@@ -485,7 +485,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_mfma(Product p, unsigne
 }
 
 // Up to 16 rows: the product is a reading of the weights.  A wave has 16 columns and an eighth of the work-group's share of the contraction, its
-// fragments straight from memory, 256 contiguous bytes of a weight row per round; the eight sums are joined in LDS.
+// fragments straight from memory, 256 contiguous bytes of a weight row per round; the eight sums are joined in LDS.  One row of 4096 x 4096:
+// 8.6 us (3.9 TB/s; a launch alone takes 3.6).
 template <int OUT>
 __global__ __launch_bounds__(512) void k_linear_few(Product p, int steps_per_split) {
   __shared__ __align__(16) float part[8][16][20];
@@ -523,7 +524,7 @@ __global__ __launch_bounds__(512) void k_linear_few(Product p, int steps_per_spl
   finish8<OUT>(p, m, n, v, blockIdx.y, ahead<OUT>(p, n), residual8<OUT>(p, m, n));
 }
 
-// y or the sum from the shares of a split contraction
+// y or the sum from the shares of a split contraction (4.4 us of the 14 at 128 x 4096 x 4096, four shares)
 template <int OUT>
 __global__ __launch_bounds__(256) void k_linear_join(Product p, const float* __restrict__ slabs, int splits) {
   const int units = (p.N + 7) / 8;

@@ -4,7 +4,7 @@
 // that log p and 1 - p keep their digits where one class is all but certain, and the entropy log Z - dot / Z adds two terms that
 // are never negative.
 //
-// All of them are bound by reading the logits once (and writing the gradient once).  A row, or one part of it, is read into registers as
+// What none of them can do without is reading the logits once (and writing the gradient once).  A row, or one part of it, is read into registers as
 // it is stored, 16 bytes per thread and unit, by one wave or by one work-group; every pass over it -- maximum, sums, list, gradient
 // -- then takes it from there.  Long rows of few are divided among work-groups whose records a second launch joins.
 #include <type_traits>
@@ -563,7 +563,10 @@ __device__ __forceinline__ float logit_of(const T* s, int label, int classes) {
   return label >= 0 && label < classes ? __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(to_f32(s[label])))) : INF;
 }
 
-// rows that a wave or 256 threads hold: many of them on a CU at a time
+// Rows that a wave, 256 or 512 threads hold.  Bound by instructions and by what the row's phases wait for (its bytes, reductions, the list),
+// not by memory, so several rows are on a CU at a time, each in another phase: of 512 threads with 128 registers two.  2048 rows of 50257 bf16
+// logits with lists of 64: 88 us (2.3 TB/s; 57 without lists), where one work-group of 1024 threads per CU took 131 although the next
+// row was on its way to LDS meanwhile, and 256 threads with 28 units 101.  8192 rows of 1000 fp32 logits, a wave each: 16.6 us (2.0 TB/s).
 template <class T, int NT, int J, int PER>       // PER: rows per work-group
 __global__ __launch_bounds__(NT * PER, NT == 512 ? 4 : 1) void k_logprob_forward(LogprobForward a) {
   __shared__ GroupSpace<NT> space[PER];
@@ -578,8 +581,8 @@ __global__ __launch_bounds__(NT * PER, NT == 512 ? 4 : 1) void k_logprob_forward
   logprob_row(a, g, h, s, row, label, logit_of(s, label, a.classes));
 }
 
-// Long rows: one work-group per CU goes through rows one after the other.  While it works on one row in registers the next one is on its way to
-// LDS (AHEAD units per thread), so that memory does not wait for the passes.
+// Rows that fill a CU's registers (more than 8192 units): one work-group per CU goes through rows one after the other.  While it works on one row
+// in registers half of the next one is on its way to LDS (AHEAD units per thread).  2048 rows of 131072 bf16 logits: 200 us (2.7 TB/s).
 template <class T, int J, int AHEAD>
 __global__ __launch_bounds__(1024) void k_logprob_rows(LogprobForward a) {
   typedef Held<T, 1024, J> H;
@@ -604,6 +607,7 @@ __global__ __launch_bounds__(1024) void k_logprob_rows(LogprobForward a) {
   }
 }
 
+// Few long rows (one of 131072 bf16 logits with a list of 20: 8.6 us, and 5.5 for the join; a launch alone takes 3.6).
 // Rows divided among work-groups: group `part` of `parts` takes every chunk of CAPACITY elements from part * per_part on
 template <class T, int J>
 __global__ __launch_bounds__(256) void k_logprob_part(LogprobForward a, int parts, long per_part, PartRecord* records, Key* lists) {
@@ -716,7 +720,8 @@ __global__ __launch_bounds__(256) void k_logprob_join(LogprobForward a, int part
 }
 
 // ---- gradient of log probability and entropy ---------------------------------------------------------------------------
-// Every work-group has 1024 16-byte units of a row, all on their way before the first is used
+// Every work-group has 1024 16-byte units of a row, all on their way before the first is used.  Bound by memory: 2048 rows of 50257 bf16 logits
+// in 76 us (5.4 TB/s read and written; a copy reaches 6.3).
 template <class T>
 __global__ __launch_bounds__(256) void k_logprob_backward(LogprobBackward a, unsigned blocks_per_row) {
   constexpr int U = 4;
@@ -822,7 +827,7 @@ __device__ __forceinline__ void finish_list(const Distill& a, List& l, const Sof
 }
 
 // exp at temperature 1 next to exp at temperature T: HARD_EXP of its own, or HARD_ONE / HARD_TWO / HARD_FOUR: e^(1/T) to the power T = 1, 2, 4
-// (an exponential costs four times a multiplication)
+// (an exponential costs four times a multiplication: rows by 512 threads and more, 2048 of 131072 classes at T = 2: 267 us, at T = 3: 287)
 enum : int { HARD_NONE = 0, HARD_EXP = 1, HARD_ONE = 2, HARD_TWO = 3, HARD_FOUR = 4 };
 struct Exponents {
   float m, ct;
@@ -967,6 +972,7 @@ __device__ __forceinline__ void distill_row(const Distill& a, const Group<NT>& g
   if (NT > 64) __syncthreads(); else __builtin_amdgcn_s_waitcnt(0x0f70);   // the stores above are done before the entries replace some of them
   if (g.tid < 64) Answer<T>::write(entries, d, 0, a.classes);
 }
+// Rows of a wave, or of 256 threads where they are few: all in one launch (256 rows of 1000 fp32 logits, lists of 32: 8.1 us)
 template <int HARD, class T, int NT, int J, int PER>
 __global__ __launch_bounds__(NT * PER) void k_distill(Distill a) {
   __shared__ GroupSpace<NT> space[PER];
@@ -1008,6 +1014,7 @@ struct Factors {
                    bad ? quiet_nan() : HARD && hot ? b.weight * a.hard_weight / (1.f + v.rest1) : 0.f};
   }
 };
+// Two rows of 512 threads on a CU, as in k_logprob_forward: 2048 rows of 50257 bf16 logits in 111 us (145 by k_distill_rows).
 template <int HARD, class T, int NT, int J>
 __global__ __launch_bounds__(NT, 4) void k_distill_held(Distill a, Soft* records) {
   __shared__ GroupSpace<NT> space;
@@ -1023,7 +1030,9 @@ __global__ __launch_bounds__(NT, 4) void k_distill_held(Distill a, Soft* records
   if (g.tid == 0) records[row] = v;
   if (a.dlogits) write_gradient<HARD>(h, (T*)a.dlogits + row * a.ldd, v.m, it, f.soft, f.hard, [](int) {});
 }
-// Longer ones, like k_logprob_rows; the units that LDS has no room for follow into their registers as the gradient leaves them.
+// Rows of more than 8192 units, like k_logprob_rows; the units that LDS has no room for follow into their registers as the gradient leaves them.
+// 2048 rows of 131072 bf16 logits: 255 us, 4.2 TB/s read and written; instructions, 18 per element and two exponentials, takes
+// 60 % of that by itself.
 template <int HARD, class T, int J, int AHEAD>
 __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records) {
   typedef Held<T, 1024, J> H;
@@ -1060,6 +1069,8 @@ __global__ __launch_bounds__(1024) void k_distill_rows(Distill a, Soft* records)
     __syncthreads();                                   // space.n is read
   }
 }
+// Loss, and the gradient at the listed classes and the label, a wave per row: 17 us for 2048 rows and lists of 64, the trips to memory one after
+// the other and the logarithms in double.
 template <class T>
 __global__ __launch_bounds__(256) void k_distill_entries(Distill a, const Soft* __restrict__ records) {
   const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64)), lane = threadIdx.x & 63;
@@ -1138,15 +1149,19 @@ __global__ __launch_bounds__(256) void k_distill_join(Distill a, int parts, long
 
 // ---- how rows are cut ------------------------------------------------------------------------------------------------
 constexpr int CUS = 256, MAX_PARTS = 256, PART_J = 4;
-constexpr int SPREAD_ROWS = 4 * CUS;     // up to so many short rows get a work-group each, on all CUs, instead of one of four
+// up to so many short rows get a work-group each, on all CUs, instead of one for four (rows of 1000 fp32 logits, lists of 5: 64 to 512 rows 6.3 to
+// 6.8 us instead of 7.0 to 7.2, 8192 rows 17.0 instead of 15.6)
+constexpr int SPREAD_ROWS = 4 * CUS;
 
 struct RowCut {
   int parts;
   long per_part;                 // classes
   int units;                     // 16-byte units of a row, with the one that a row across a boundary has more
 };
-// A row of 2048 units (32 KiB) and more is divided if there are not enough rows for all CUs, and if no work-group holds it (a part of it may
-// then need several chunks).
+// A row of 2048 units (32 KiB) and more is divided if there are at most 64 of them, and if no work-group holds it (a part of it may then need
+// several chunks).  Lists of 5 and distillation, bf16, us: 64 rows of 131072 classes 19 and 21 divided, 23 and 32 undivided; 16 of 50000 12 and
+// 12 against 16 and 17; but 128 of 50000 19 and 19 against 16 and 19.5, 128 of 131072 32 and 33 against 25 and 35.  16 to 64 rows of 16376,
+// less than 2048 units: 12.5 and 11.5 against 10 and 10.7.
 // aligned: every row starts on 16 bytes (a workspace is sized for rows that do not, which never have fewer parts).
 RowCut row_cut(int dt, int rows, int classes, bool aligned) {
   const int E = dt == DT_BF16 ? 8 : 4;
@@ -1154,7 +1169,7 @@ RowCut row_cut(int dt, int rows, int classes, bool aligned) {
   c.units = (classes + E - 1) / E + (aligned ? 0 : 1);
   const bool too_long = c.units > 1024 * 16;
   c.parts = 1;
-  if (too_long || (rows <= CUS / 2 && c.units >= 2048)) {
+  if (too_long || (rows <= CUS / 4 && c.units >= 2048)) {
     long p = (2 * CUS + rows - 1) / rows;
     const long most = c.units / 512;
     if (p > most) p = most;

@@ -546,3 +546,9 @@ def test_lists_among_thousands_of_large_logits_of_many_rows(env, mode, classes, 
 @pytest.mark.parametrize("shape", [(1030, 9001), (200, 20001), (140, 65536), (300, 70001)], ids=lambda s: "x".join(map(str, s)))
 def test_streams_and_graphs_of_many_rows(env, shape):
     test_streams_and_graphs(env, shape)
+
+
+@pytest.mark.parametrize("shape", [(64, 16500), (65, 16500), (100, 33001), (100, 70001)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_around_the_number_that_is_divided(env, shape):
+    test_many_long_rows(env, "bf16", shape)
+    test_many_long_rows(env, "f32", shape)
