@@ -56,63 +56,91 @@ struct Epilogue {
 
 // fp32 (check mode): C tile of 32 x 32 by eight waves, four of 16 x 16 for each half of the 64 steps that are staged at a time; the halves are
 // joined at the end.  v_mfma_f64_16x16x4_f64 takes 64 cycles, so small tiles, which give every CU one, cost nothing: 333 x 1000 x 517 has 187 of
-// them (64 x 64 ones with four waves: 54, and 144 us instead of 26, a fifth of the rate of a large product in double).  Any sizes and strides.
+// them (64 x 64 ones with four waves: 54, and 144 us instead of 25, a fifth of the rate of a large product in double).  Any sizes and strides.
 __global__ __launch_bounds__(512) void k_linear_tile_f32(Operand A, Operand B, Epilogue e, int M, int N, int K) {
   constexpr int KS = 64, LS = KS + 4;
-  __shared__ __align__(16) float sA[32 * LS], sB[32 * LS];
+  __shared__ __align__(16) float sA[2][32 * LS], sB[2][32 * LS];
   __shared__ double join[4][64][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = wave >> 2;
   const unsigned cols = (unsigned)(N + 31) / 32;
   const int m0 = (int)(blockIdx.x / cols) * 32, n0 = (int)(blockIdx.x % cols) * 32;
   const int wm = (wave & 1) * 16, wn = (wave >> 1 & 1) * 16;
   doublex4 acc = {0.0, 0.0, 0.0, 0.0};
-  float ra[4], rb[4];
-  // a thread's four elements of an operand's 32 x 64: along whichever of row and k is contiguous
-  auto at = [&](const Operand& o, int i, int& r, int& k) {
-    if (o.ks == 1) { r = tid >> 4; k = (tid & 15) * 4 + i; }
-    else { r = tid & 31; k = (tid >> 5) + 16 * i; }
+  float ra[2][4], rb[2][4];
+  // A thread's four elements of an operand's 32 x 64: along whichever of row and k is contiguous.  Rows behind the last one read the last one, for
+  // results that nobody stores.  In the step where the contraction ends, elements behind the end read the first one of the row and become 0 on the
+  // way to LDS.  No load stands behind a condition or is looked at before, so nobody waits for it before it is due.
+  struct Side { const float* p; long ks; int r, k, dk; bool vec; } a, b;
+  auto side = [&](const Operand& o, int r0, int rows) {
+    Side s;
+    const bool along = o.ks == 1;
+    s.r = along ? tid >> 4 : tid & 31;
+    s.k = along ? (tid & 15) * 4 : tid >> 5;
+    s.dk = along ? 1 : 16;
+    s.ks = o.ks;
+    s.p = o.p + (long)(r0 + s.r < rows ? r0 + s.r : rows - 1) * o.rs;
+    s.vec = along && ((uintptr_t)o.p & 15) == 0 && (o.rs & 3) == 0;
+    return s;
   };
-  auto load = [&](const Operand& o, int r0, int rows, int k0, float (&v)[4]) {
-    int r, k;
-    at(o, 0, r, k);
-    if (o.ks == 1 && r0 + r < rows && k0 + k + 4 <= K) {
-      const float* p = o.p + (long)(r0 + r) * o.rs + k0 + k;
-      if (((uintptr_t)p & 15) == 0) {
-        const float4 q = *reinterpret_cast<const float4*>(p);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-        return;
-      }
-    }
+  a = side(A, m0, M);
+  b = side(B, n0, N);
+  const float *next_a = a.p + a.k * a.ks, *next_b = b.p + b.k * b.ks;
+  auto load = [&](const Side& s, const float*& next, int k0, float (&v)[4]) {
+    if (k0 + KS > K) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      at(o, i, r, k);
-      v[i] = r0 + r < rows && k0 + k < K ? o.p[(long)(r0 + r) * o.rs + (long)(k0 + k) * o.ks] : 0.f;
+      for (int i = 0; i < 4; ++i) v[i] = s.p[k0 + s.k + i * s.dk < K ? (k0 + s.k + i * s.dk) * s.ks : 0];
+      return;
     }
-  };
-  auto put = [&](const Operand& o, float* s, const float (&v)[4]) {
+    if (s.vec) {
+      const float4 q = *reinterpret_cast<const float4*>(next);
+      v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      int r, k;
-      at(o, i, r, k);
-      s[r * LS + k] = v[i];
+      for (int i = 0; i < 4; ++i) v[i] = next[i * s.dk * s.ks];
+    }
+    next += KS * s.ks;
+  };
+  auto put = [&](const Side& s, float* to, int k0, float (&v)[4]) {
+    if (k0 + KS > K)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k0 + s.k + i * s.dk >= K) v[i] = 0.f;
+    if (s.dk == 1) {
+      *reinterpret_cast<float4*>(to + s.r * LS + s.k) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[s.r * LS + s.k + 16 * i] = v[i];
     }
   };
-  load(A, m0, M, 0, ra);
-  load(B, n0, N, 0, rb);
-  for (int k0 = 0; k0 < K; k0 += KS) {
+  auto step = [&](int k0, auto set) {        // the registers of a step have been loaded two steps before
+    constexpr int S = decltype(set)::value;
+    put(a, sA[S], k0, ra[S]);
+    put(b, sB[S], k0, rb[S]);
+    if (k0 + 2 * KS < K) {
+      load(a, next_a, k0 + 2 * KS, ra[S]);
+      load(b, next_b, k0 + 2 * KS, rb[S]);
+    }
     __syncthreads();
-    put(A, sA, ra);
-    put(B, sB, rb);
-    __syncthreads();
-    if (k0 + KS < K) {
-      load(A, m0, M, k0 + KS, ra);
-      load(B, n0, N, k0 + KS, rb);
-    }
+    float fa[KS / 8], fb[KS / 8];             // all fragments asked for ahead of the products
 #pragma unroll
-    for (int k = 0; k < KS / 2; k += 4) {
-      const int c = part * (KS / 2) + k + (lane >> 4);
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)sB[(wn + (lane & 15)) * LS + c], (double)sA[(wm + (lane & 15)) * LS + c], acc, 0, 0, 0);
+    for (int i = 0; i < KS / 8; ++i) {
+      const int c = part * (KS / 2) + i * 4 + (lane >> 4);
+      fa[i] = sA[S][(wm + (lane & 15)) * LS + c];
+      fb[i] = sB[S][(wn + (lane & 15)) * LS + c];
     }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < KS / 8; ++i) acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)fb[i], (double)fa[i], acc, 0, 0, 0);
+  };
+  load(a, next_a, 0, ra[0]);
+  load(b, next_b, 0, rb[0]);
+  if (KS < K) {
+    load(a, next_a, KS, ra[1]);
+    load(b, next_b, KS, rb[1]);
+  }
+  for (int k0 = 0; k0 < K; k0 += 2 * KS) {
+    step(k0, std::integral_constant<int, 0>{});
+    if (k0 + KS < K) step(k0 + KS, std::integral_constant<int, 1>{});
   }
   if (part)
 #pragma unroll
