@@ -381,3 +381,9 @@ def test_columns_of_one_matrix(env, mode):
 @pytest.mark.parametrize("shape", [(4100, 264, 2600), (300, 2560, 4104), (16, 1000, 30000)], ids=lambda s: "x".join(map(str, s)))
 def test_streams_and_graphs_on_the_largest_tiles(env, shape):
     test_streams_and_graphs(env, shape)
+
+
+@pytest.mark.parametrize("shape", [(1 << 21, 3, 2), (1 << 21, 64, 8), (1, 1 << 20, 4), (17, 1 << 20, 8), (2, 5, 1 << 20), (33, 8, 1 << 20)], ids=lambda s: "x".join(map(str, s)))
+def test_largest_sizes(env, shape):
+    test_forward_every_activation(env, "bf16", shape)
+    test_backward(env, "bf16", shape)

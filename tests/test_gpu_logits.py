@@ -48,10 +48,14 @@ class Row64:
         self.m = s.amax(1, keepdim=True)
         self.t = (s - self.m) * scale
         e = self.t.exp()
-        self.z = e.sum(1, keepdim=True)
-        self.logp = self.t - self.z.log()
-        self.p = e / self.z
-        self.tail = 1 - self.p.amax(1, keepdim=True)           # rest / Z
+        # 1 + rest, rest without the largest: log(1 + rest) of a rounded sum would be off by 2^-53, more than the kernels' error where
+        # rest is 1e-12
+        rest = e.scatter(1, self.t.argmax(1, keepdim=True), 0.0).sum(1, keepdim=True)
+        rest = torch.where(self.m.isinf(), math.nan, rest)
+        self.logz = torch.log1p(rest)
+        self.logp = self.t - self.logz
+        self.p = e / (1 + rest)
+        self.tail = rest / (1 + rest)
         # relative to rest = sum' e_i (without the largest): sum' e_i (|t_i| + 4) 2^-23 / sum' e_i, where sum' e_i |t_i| / sum' e_i is
         # sum p_i |t_i| / tail, since the largest has t = 0
         size = (self.p * self.t.clamp(min=-1e30).abs()).sum(1, keepdim=True) / self.tail.clamp(min=1e-300)
@@ -81,7 +85,7 @@ def check_forward(torch, s, labels, top, r):
     near(r.entropy, q.entropy[:, 0], (q.rel * (2 * q.entropy + q.tail) + 1e-30)[:, 0], "entropy")
     assert torch.equal(r.rank, before(torch, s, labels))
     near(r.stats[:, :1], q.m, 0 * q.m, "maximum")
-    near(r.stats[:, 1:], q.z.log(), tol(q.z.log()), "log sum")
+    near(r.stats[:, 1:], q.logz, tol(q.logz), "log sum")
     if top:
         value, index = torch.sort(s.double(), dim=1, descending=True, stable=True)
         n = min(top, s.shape[1])
@@ -552,3 +556,15 @@ def test_streams_and_graphs_of_many_rows(env, shape):
 def test_rows_around_the_number_that_is_divided(env, shape):
     test_many_long_rows(env, "bf16", shape)
     test_many_long_rows(env, "f32", shape)
+
+
+@pytest.mark.parametrize("shape", [(1 << 21, 1), (1 << 21, 3), (1, 1 << 28)], ids=lambda s: "x".join(map(str, s)))
+def test_largest_sizes(env, shape):
+    hpf, torch, ops = env
+    print(f"\n[case] largest {shape}", flush=True)
+    s, labels, g = make(torch, "bf16", *shape)
+    r = ops["bf16"].logprob_forward(s, labels, 5)
+    check_forward(torch, s, labels, 5, r)
+    index, logit = r.top_index, torch.where(r.top_index < 0, 0.0, r.top_logprob)
+    loss, ds = ops["bf16"].distill(s, index, logit, labels, temperature=2.0, hard_weight=0.5)
+    check_distill(torch, "bf16", s, index, logit, labels, 2.0, 0.5, None, loss, ds)
