@@ -3,6 +3,7 @@
 // Every launcher only enqueues work on `stream` and returns hipGetLastError().
 #pragma once
 #include "hpf_kernels.h"
+#include "hpf_linear_cut.h"
 
 namespace hpf {
 
@@ -31,7 +32,6 @@ struct LinearBackward {
   int M, K, N;
 };
 
-inline int round_up64(int v) { return (v + 63) / 64 * 64; }
 // Packed weights: bf16 [N][Kp] (forward operand), then bf16 [K][Np] (operand of dx), rows padded with zeros
 inline size_t linear_packed_elems(int K, int N) { return (size_t)N * round_up64(K) + (size_t)K * round_up64(N); }
 hipError_t launch_linear_pack(const float* w, bf16_t* packed, int K, int N, hipStream_t stream);

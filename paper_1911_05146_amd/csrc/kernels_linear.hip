@@ -210,8 +210,6 @@ __device__ __forceinline__ void activate_fast(int act, float z, float& y, float&
   }
 }
 
-__host__ __device__ constexpr int slab_row(int n) { return (n + 7) & ~7; }       // rows of partial sums start on 32 bytes
-
 // Eight consecutive results of a row, n a multiple of 8.  The bias and, where rows allow 16-byte loads, the residual are asked for ahead of the
 // sums they join: one at a time they cost a trip to memory for every 16 rows of a tile.  With residual, bias, gelu and slope
 // 8192 x 4096 x 4096 takes 254 us, 54 of them on top of the product; their bytes alone take 32.
@@ -519,7 +517,7 @@ template <int OUT>
 __global__ __launch_bounds__(512) void k_linear_few(Product p, int steps_per_split) {
   __shared__ __align__(16) float part[8][16][20];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, q = lane >> 4;
-  const int n0 = blockIdx.x * 16, k_all = (p.K + 31) / 32;
+  const int n0 = blockIdx.x * 16, k_all = round_up64(p.K) / 32;
   const int k_begin = (int)blockIdx.y * steps_per_split, k_end = k_begin + steps_per_split < k_all ? k_begin + steps_per_split : k_all;
   const int share = ((k_end - k_begin + 7) / 8 + 3) & ~3, k0 = k_begin + wave * share, k1 = k0 + share < k_end ? k0 + share : k_end;
   const bf16_t* a = p.A + (row < p.M ? row : p.M - 1) * p.lda + q * 8;
@@ -720,40 +718,6 @@ unsigned grid_for(size_t n, size_t per, size_t cap) {
   const size_t g = (n + per - 1) / per;
   return (unsigned)(g < 1 ? 1 : g > cap ? cap : g);
 }
-size_t align256(size_t v) { return (v + 255) / 256 * 256; }
-
-// How a bf16 product is cut (M x K x N, us):
-// - 256 x 256 tiles where there are 160 (2560 x 4096 x 4096, 160 tiles: 84, with 128 x 128 ones 97; 2048 x 4096 x 4096, 128 tiles: 78 and 67);
-// - 128 x 128 ones where there are 256 (2048 x 4096 x 2048, 256 tiles: 52, with 64 x 64 ones 61; 1536 x 4096 x 1536, 144 tiles: 42 and 37);
-// - 64 x 64 ones, two work-groups of four stages per CU, with the contraction split until there is a work-group per CU;
-// - k_linear_few for up to 16 rows of small weights, where a launch less counts most.  It reads K N weights once and x again for every 16
-//   columns, K N M / 16, and takes up to 1.25 * 2^25 of both (4096 x 4096: 13.2 to 11.9 for 1 to 16 rows, with 64 x 64 tiles 14.5 to 13.9;
-//   4096 x 8192: 13.0 and 14.6 for one row, 17.4 and 15.1 for 16; 4096 x 32000: 40 and 37, 58 and 37).
-enum : int { CUT_LARGE, CUT_TILES, CUT_SPLIT, CUT_FEW };
-struct Cut {
-  int kind, splits, steps;      // steps (of 64, CUT_FEW: 32) per share
-  unsigned rows, cols;          // tiles
-};
-Cut cut_of(int M, int N, int K, bool rows) {      // rows: of a ROWS product
-  auto tiles = [&](int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  Cut c;
-  const bool few = M <= 16 && !rows && (long)K * N * (16 + M) <= 20l << 25;
-  c.kind = few ? CUT_FEW : tiles(256, 256) >= 160 ? CUT_LARGE : tiles(128, 128) >= 256 ? CUT_TILES : CUT_SPLIT;
-  const int bm = c.kind == CUT_FEW ? 16 : c.kind == CUT_LARGE ? 256 : c.kind == CUT_TILES ? 128 : 64, bn = bm;
-  c.rows = (unsigned)((M + bm - 1) / bm);
-  c.cols = (unsigned)((N + bn - 1) / bn);
-  const int unit = c.kind == CUT_FEW ? 32 : 64, k = (K + unit - 1) / unit, least = c.kind == CUT_FEW ? 32 : 8;
-  long want = c.kind == CUT_SPLIT || c.kind == CUT_FEW ? 256 / ((long)c.rows * c.cols) : 1;
-  if (want > k / least) want = k / least;
-  if (want < 1) want = 1;
-  c.steps = (int)((k + want - 1) / want);
-  c.splits = (k + c.steps - 1) / c.steps;
-  return c;
-}
-size_t slab_bytes(int M, int N, int K, bool rows) {
-  const Cut c = cut_of(M, N, K, rows);
-  return c.splits > 1 ? align256((size_t)c.splits * M * slab_row(N) * sizeof(float)) : 0;
-}
 
 template <int BM, int BN, int WM, int WN, int STAGES, int OUT, bool ROWS>
 hipError_t mfma(const Product& p, const Cut& c, hipStream_t s) {
@@ -772,11 +736,10 @@ hipError_t few(const Product& p, const Cut& c, hipStream_t s) {
   return hipGetLastError();
 }
 
-// y, or (ROWS) a sum; slabs: room for slab_bytes
+// y, or (ROWS) a sum; slabs: room for slab_bytes(c, ...)
 template <bool ROWS>
-hipError_t product(const Product& p, float* slabs, hipStream_t s) {
+hipError_t product(const Product& p, const Cut& c, float* slabs, hipStream_t s) {
   constexpr int OUT = ROWS ? OUT_SUM : OUT_Y;
-  const Cut c = cut_of(p.M, p.N, p.K, ROWS);
   if (c.kind == CUT_LARGE) return mfma<256, 256, 2, 4, 2, OUT, ROWS>(p, c, s);
   if (c.kind == CUT_TILES) return mfma<128, 128, 2, 2, 2, OUT, ROWS>(p, c, s);
   if (c.splits == 1) {
@@ -797,9 +760,6 @@ hipError_t product(const Product& p, float* slabs, hipStream_t s) {
 // Rows that the tiles read where they are: 16-byte units, and 256 rows within 32-bit offsets
 bool direct(const void* p, long ld, int K) { return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (K & 7) == 0 && ld <= 1 << 22; }
 
-// Rows in a work-group of k_linear_rows: 64, or 16 while that gives no CU two work-groups (gradients of 1021 x 2049 x 1000: 47.8 us
-// with 64, 43.6 with 16; of 8192 x 4096 x 4096, where 64 it is, no difference, but a quarter of the sums)
-int group_of(int M, int width) { return (long)((M + 63) / 64) * ((width + 511) / 512) >= 512 ? 64 : 16; }
 unsigned row_blocks(const Rows& r) { return (unsigned)((r.M + r.group - 1) / r.group) * (unsigned)((r.ld + 511) / 512); }
 // a copy whose rows start on 16 bytes
 Rows copy_of(const void* x, long ldx, int M, int K, char* to) {
@@ -808,6 +768,7 @@ Rows copy_of(const void* x, long ldx, int M, int K, char* to) {
 }
 
 hipError_t forward_bf16(const LinearForward& a, char* ws, hipStream_t s) {
+  const ForwardSpace at(a.M, a.K, a.N);
   Product p{};
   p.A = (const bf16_t*)a.x; p.lda = a.ldx; p.M = a.M; p.N = a.N; p.K = a.K;
   if (!direct(a.x, a.ldx, a.K)) {
@@ -817,28 +778,10 @@ hipError_t forward_bf16(const LinearForward& a, char* ws, hipStream_t s) {
     if (e != hipSuccess) return e;
     p.A = r.dst; p.lda = p.K = r.ld;
   }
-  ws += align256((size_t)a.M * round_up64(a.K) * 2);
   p.B = (const bf16_t*)a.weights; p.ldb = round_up64(a.K);
   p.bias = a.bias; p.residual = (const bf16_t*)a.residual; p.ldr = a.ldr; p.y = (bf16_t*)a.y; p.ldy = a.ldy; p.slope = (bf16_t*)a.slope; p.act = a.act;
-  return product<false>(p, (float*)ws, s);
+  return product<false>(p, at.y, (float*)(ws + at.slabs), s);
 }
-
-// Workspace of a backward call: dz [M][Np] | x [M][Kp] | sums of groups of rows [groups][N] | shares of a split product
-struct BackwardSpace {
-  size_t dz, x, sums, slabs, bytes;
-  int group, groups;            // rows of a sum; sums
-  BackwardSpace(int M, int K, int N) {
-    const size_t Kp = round_up64(K), Np = round_up64(N);
-    dz = 0;
-    group = group_of(M, (int)Np);
-    groups = (M + group - 1) / group;
-    x = align256((size_t)M * Np * 2);
-    sums = x + align256((size_t)M * Kp * 2);
-    slabs = sums + align256((size_t)groups * N * 4);
-    const size_t d = slab_bytes(M, K, (int)Np, false), w = slab_bytes(K, N, M, true);
-    bytes = slabs + (d > w ? d : w);
-  }
-};
 
 hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
   const BackwardSpace at(a.M, a.K, a.N);
@@ -866,7 +809,7 @@ hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
     p.B = (const bf16_t*)a.weights + (size_t)a.N * round_up64(a.K); p.ldb = Np;
     p.M = a.M; p.N = a.K; p.K = copy ? Np : a.N;
     p.y = (bf16_t*)a.dx; p.ldy = a.lddx;
-    e = product<false>(p, (float*)(ws + at.slabs), s);
+    e = product<false>(p, at.dx, (float*)(ws + at.slabs), s);
   }
   if (e == hipSuccess && a.dw) {
     Product p{};
@@ -874,7 +817,7 @@ hipError_t backward_bf16(const LinearBackward& a, char* ws, hipStream_t s) {
     p.widthA = copy_x ? x.ld : a.K;
     p.B = dz; p.ldb = lddz; p.widthB = copy ? Np : a.N;
     p.M = a.K; p.N = a.N; p.K = a.M; p.sum = a.dw; p.accumulate = a.accumulate;
-    e = product<true>(p, (float*)(ws + at.slabs), s);
+    e = product<true>(p, at.dw, (float*)(ws + at.slabs), s);
   }
   return e;
 }
@@ -926,7 +869,7 @@ hipError_t launch_linear_pack(const float* w, bf16_t* packed, int K, int N, hipS
 
 size_t linear_workspace_bytes(int dt, int M, int K, int N) {
   if (dt != DT_BF16) return (size_t)M * N * sizeof(float);
-  const size_t f = align256((size_t)M * round_up64(K) * 2) + slab_bytes(M, N, round_up64(K), false), b = BackwardSpace(M, K, N).bytes;
+  const size_t f = ForwardSpace(M, K, N).bytes, b = BackwardSpace(M, K, N).bytes;
   return f > b ? f : b;
 }
 

@@ -1,0 +1,83 @@
+"""GPU tests at the edges of the operators at the answer end of a model: workspaces of exactly the size asked for, with a guard behind them.
+
+Tolerances: a sum of n products in fp32 is off by at most n 2^-24 sum |a_i b_i|, a result in bf16 is rounded once by half a step, 2^-8 of it."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: these tests need a real MI355X")
+    from paper_1911_05146_amd import hpf
+    return hpf, torch
+
+
+def randn(torch, seed, *shape):
+    return torch.randn(*shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+def check(got, ref, tol, what):
+    bad = ~((got.double() - ref).abs() <= tol)
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()} off"
+
+
+class Guarded:
+    """A workspace of exactly `need` bytes, filled with NaN, and 64 KiB behind it that nobody may touch."""
+
+    def __init__(self, torch, need):
+        self.need = need
+        self.raw = torch.full((need + 65536 + 256,), 0xff, device="cuda", dtype=torch.uint8)
+        self.at = -self.raw.data_ptr() % 256
+        self.ptr = self.raw.data_ptr() + self.at
+        self.raw[self.at + need:] = 0xa5
+
+    def check(self):
+        assert bool((self.raw[self.at + self.need:] == 0xa5).all()), "written behind the workspace"
+
+
+# up to 16 rows and long contractions, where the number of shares depends on how the contraction is counted; then every other cut
+FEW = [(16, 89760, 40), (16, 89760, 48), (1, 53856, 65), (5, 53856, 65), (1, 89736, 40), (3, 40, 48)]
+CUTS = FEW + [(16, 4096, 4096), (1, 40, 89760), (16, 40, 89760), (128, 4096, 512), (40, 2600, 4104), (130, 2565, 999), (2560, 512, 4096), (1021, 257, 1000)]
+
+
+@pytest.mark.parametrize("M,K,N", CUTS)
+def test_products_stay_within_a_workspace_of_the_size_asked_for(env, M, K, N):
+    hpf, torch = env
+    print(f"\n[case] workspace {M}x{K}x{N}", flush=True)
+    bf16 = torch.bfloat16
+    x, w, dy = randn(torch, 1, M, K).to(bf16), randn(torch, 2, K, N) * K ** -0.5, randn(torch, 3, M, N).to(bf16)
+    slope = randn(torch, 4, M, N).to(bf16)
+    weights = hpf.Ops(hpf.HPF_BF16).linear_weights(w)
+    seen = w.to(bf16).double()
+    need = hpf.hpf_op_linear_workspace_bytes(hpf.HPF_BF16, M, K, N)
+    stream = torch.cuda.current_stream().cuda_stream
+    # rows in place, and rows that are copied because they start off 16 bytes
+    wide = torch.empty(M, K + 1, device="cuda", dtype=bf16)
+    wide[:, 1:] = x
+    sums = []
+    for a, lda in ((x, K), (wide[:, 1:], K + 1)):
+        ws = Guarded(torch, need)
+        y = torch.empty(M, N, device="cuda", dtype=bf16)
+        hpf.hpf_op_linear_forward(hpf.HPF_BF16, a.data_ptr(), lda, weights.ptr, 0, 0, 0, y.data_ptr(), N, 0, M, K, N, hpf.HPF_ACT_NONE, ws.ptr, need, stream)
+        torch.cuda.synchronize()
+        ws.check()
+        ref = x.double() @ seen
+        check(y, ref, 2.0 ** -8 * 1.01 * ref.abs() + (K + 8) * 2.0 ** -24 * (x.double().abs() @ seen.abs()), "y")
+        sums.append(y)
+    assert torch.equal(*sums), "the copy of the rows gives other bits"
+    for sl in (None, slope):
+        dz = dy.double() if sl is None else (dy.double() * sl.double()).to(bf16).double()
+        ws = Guarded(torch, need)
+        dx, dw, db = torch.empty(M, K, device="cuda", dtype=bf16), torch.empty(K, N, device="cuda"), torch.empty(N, device="cuda")
+        hpf.hpf_op_linear_backward(hpf.HPF_BF16, dy.data_ptr(), N, x.data_ptr(), K, weights.ptr, 0 if sl is None else sl.data_ptr(), dx.data_ptr(), K, dw.data_ptr(),
+                                   db.data_ptr(), 0, M, K, N, ws.ptr, need, stream)
+        torch.cuda.synchronize()
+        ws.check()
+        ref = dz @ seen.t()
+        check(dx, ref, 2.0 ** -8 * 1.01 * ref.abs() + (N + 8) * 2.0 ** -24 * (dz.abs() @ seen.t().abs()) + 1e-38, "dx")
+        ref, size = x.double().t() @ dz, x.double().t().abs() @ dz.abs()
+        check(dw, ref, 2.0 ** -24 * 1.01 * ref.abs() + (M + 8) * 2.0 ** -24 * size + 1e-38, "dw")
+        check(db, dz.sum(0), 2.0 ** -24 * 1.01 * dz.sum(0).abs() + (M + 8) * 2.0 ** -24 * dz.abs().sum(0) + 1e-38, "db")
