@@ -823,7 +823,10 @@ __device__ __forceinline__ void finish_list(const Distill& a, List& l, const Sof
     }
     logp = log(p);
   }
-  l.diff = p != 0.0 ? p * expm1(logq - logp) : exp(logq);
+  // by the difference of the logarithms only where the two are close: expm1 overflows where p is a number below 2^-1022, and beyond a factor of e
+  // the subtraction loses less than a digit
+  const double d = logq - logp;
+  l.diff = fabs(d) < 1.0 ? p * expm1(d) : exp(logq) - p;
 }
 
 // exp at temperature 1 next to exp at temperature T: HARD_EXP of its own, or HARD_ONE / HARD_TWO / HARD_FOUR: e^(1/T) to the power T = 1, 2, 4
@@ -920,7 +923,7 @@ struct Answer {
     if (l.on) {
       const double hard = wh == 0.0 ? 0.0 : l.index == label ? expm1(logl) : (double)expf(l.mine - v.m) / (1.0 + (double)v.rest1);
       r.index = l.index;
-      r.at_index = (float)(ws * l.diff + wh * hard);
+      r.at_index = (float)((ws != 0.0 ? ws * l.diff : 0.0) + wh * hard);       // without weight the list has no say, as in the loss
     }
     if (has && !listed && lane == 0) {
       const double q = (double)expf((mine - v.m) * (1.f / a.temperature)) / (1.0 + (double)v.restt);

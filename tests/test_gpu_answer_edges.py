@@ -81,3 +81,41 @@ def test_products_stay_within_a_workspace_of_the_size_asked_for(env, M, K, N):
         ref, size = x.double().t() @ dz, x.double().t().abs() @ dz.abs()
         check(dw, ref, 2.0 ** -24 * 1.01 * ref.abs() + (M + 8) * 2.0 ** -24 * size + 1e-38, "dw")
         check(db, dz.sum(0), 2.0 ** -24 * 1.01 * dz.sum(0).abs() + (M + 8) * 2.0 ** -24 * dz.abs().sum(0) + 1e-38, "db")
+
+
+# every kernel of the distillation: a wave per row, few and many rows of 256 threads, rows with a second launch, long rows, divided rows
+DISTILL = [(12, 100), (1100, 300), (12, 1500), (1100, 2100), (140, 20000), (260, 131072), (2, 40000)]
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", DISTILL, ids=lambda s: "x".join(map(str, s)))
+def test_entries_of_very_small_teacher_probability(env, mode, shape):
+    """A listed class whose teacher probability is a number below 2^-1022, or none at all, gets the student's probability as its gradient."""
+    from test_gpu_logits import check_distill, distill64
+    hpf, torch = env
+    rows, classes = shape
+    print(f"\n[case] small probabilities {shape} {mode}", flush=True)
+    o = hpf.Ops(hpf.HPF_BF16 if mode == "bf16" else hpf.HPF_F32)
+    s = randn(torch, 5, rows, classes).to(o.tdtype)
+    index = torch.arange(10, device="cuda", dtype=torch.int32).repeat(rows, 1)
+    index[1::4, 9] = 8                                  # a class listed twice, each time all but impossible
+    labels = (torch.arange(rows, device="cuda") % 12 - 1).int()
+    for T in (1.0, 0.05, 2.0, 3.0):
+        gaps = torch.tensor([0.0, 1.0, 690.0, 708.0, 715.0, 720.0, 735.0, 744.0, 744.5, 800.0], device="cuda") * T
+        logit = (5.0 - gaps).repeat(rows, 1).contiguous()
+        for hw in (0.0, 0.5, 1.0):
+            loss, ds = o.distill(s, index, logit, labels, temperature=T, hard_weight=hw)
+            assert bool(loss.isfinite().all()) and bool(ds.isfinite().all()), (T, hw)
+            check_distill(torch, mode, s, index, logit, labels, T, hw, None, loss, ds)
+            if hw == 0.0:
+                at = ds.double().gather(1, index.long()[:, 2:])
+                q = torch.softmax(s.double() / float(torch.tensor(T)), 1).gather(1, index.long()[:, 2:]) * float(torch.tensor(T))
+                # relative to the value, and 2^-126 where it is less than that: there the types have no full set of digits (at T = 0.05 some are 1e-39)
+                check(at, q, (2.0 ** -7 if mode == "bf16" else 1e-4) * q + 2.0 ** -126, "the student's probability")
+    # a list that has no say (hard_weight 1) leaves loss and gradient those of the label
+    logit[0, 3], logit[rows - 1, 0] = float("nan"), float("inf")
+    loss, ds = o.distill(s, index, logit, labels, temperature=2.0, hard_weight=1.0)
+    want = o.distill(s, None, None, labels, temperature=2.0, hard_weight=1.0)
+    assert torch.equal(loss, want[0])
+    ref, dref, _ = distill64(torch, s, torch.full_like(index, -1), torch.zeros_like(logit), labels, 2.0, 1.0, None)
+    check_distill(torch, mode, s, torch.full_like(index, -1), torch.zeros_like(logit), labels, 2.0, 1.0, None, loss, ds)
