@@ -237,7 +237,7 @@ __device__ __forceinline__ void finish8(const Product& p, int m, int n, float (&
   if (OUT == OUT_SUM) {
     float* o = p.sum + (size_t)m * p.N + n;
     const bool add = p.accumulate;
-    if (left >= 8 && (p.N & 3) == 0) {
+    if (left >= 8 && (p.N & 3) == 0 && ((uintptr_t)p.sum & 15) == 0) {       // rows on 16 bytes
       if (add) {
         float w[8];
         load8(o, w);

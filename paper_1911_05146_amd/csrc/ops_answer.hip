@@ -16,6 +16,9 @@ bool type_of(hpf_dtype dtype, int& dt) {
 bool rows_ok(int64_t ld, int32_t cols) { return ld >= cols && ld <= (int64_t)1 << 40; }
 size_t elem(int dt) { return dt == DT_BF16 ? 2 : 4; }
 bool element_aligned(const void* p, int dt) { return (uintptr_t)p % elem(dt) == 0; }
+// fp32 or int32 arrays
+template <class... P>
+bool words_aligned(const P*... p) { return (((uintptr_t)p | ... | (uintptr_t)0) & 3) == 0; }
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return a && b && x < y + nb && y < x + na;
@@ -66,6 +69,7 @@ hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed
   int dt;
   const hpf_status st = linear_shape(HPF_BF16, 0, K, N, dt);
   if (st != HPF_OK) return st;
+  if (!words_aligned(w)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if ((uintptr_t)packed % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
   const size_t need = hpf_op_linear_packed_bytes(K, N);
   if (packed_bytes < need) return fail(HPF_ENOMEM, "packed weights have %zu bytes, %zu needed", packed_bytes, need);
@@ -89,7 +93,8 @@ hpf_status hpf_op_linear_forward(hpf_dtype dtype, const void* x, int64_t ldx, co
   if (M == 0) return HPF_OK;
   if (!x || !weights || !y) return fail(HPF_EINVAL, "null tensor");
   if (!rows_ok(ldx, K) || !rows_ok(ldy, N) || (residual && !rows_ok(ldr, N))) return fail(HPF_EINVAL, "row stride shorter than a row");
-  if (!element_aligned(x, dt) || !element_aligned(y, dt) || !element_aligned(residual, dt) || !element_aligned(slope, dt))
+  if (!element_aligned(x, dt) || !element_aligned(y, dt) || !element_aligned(residual, dt) || !element_aligned(slope, dt) || !words_aligned(bias) ||
+      (dt == DT_F32 && !element_aligned(weights, dt)))
     return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
   const size_t e = elem(dt);
@@ -111,6 +116,7 @@ hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy,
   hpf_status st = linear_shape(dtype, M, K, N, dt);
   if (st != HPF_OK) return st;
   hipStream_t s = (hipStream_t)hip_stream;
+  if (!words_aligned(dw, db)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (M == 0) {
     if (accumulate) return HPF_OK;
     hipError_t e = dw ? launch_zero_f32(dw, (size_t)K * N, s) : hipSuccess;
@@ -120,7 +126,8 @@ hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy,
   if (!dx && !dw && !db) return HPF_OK;
   if (!dy || (dx && !weights) || (dw && !x)) return fail(HPF_EINVAL, "null tensor");
   if (!rows_ok(lddy, N) || (dw && !rows_ok(ldx, K)) || (dx && !rows_ok(lddx, K))) return fail(HPF_EINVAL, "row stride shorter than a row");
-  if (!element_aligned(dy, dt) || !element_aligned(x, dt) || !element_aligned(dx, dt) || !element_aligned(slope, dt))
+  if (!element_aligned(dy, dt) || !element_aligned(x, dt) || !element_aligned(dx, dt) || !element_aligned(slope, dt) ||
+      (dt == DT_F32 && !element_aligned(weights, dt)))
     return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (dx && dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
   const size_t e = elem(dt);
@@ -167,6 +174,7 @@ hpf_status hpf_op_logprob_forward(hpf_dtype dtype, const void* logits, int64_t l
   if (st != HPF_OK) return st;
   if (rows == 0) return HPF_OK;
   if (top && (!top_index || !top_logprob)) return fail(HPF_EINVAL, "top_index and top_logprob are required with a list");
+  if (!words_aligned(labels, logprob, entropy, rank, stats, top_index, top_logprob)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if ((logprob || rank) && !labels) return fail(HPF_EINVAL, "labels are required for logprob and rank");
   st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
   if (st != HPF_OK) return st;
@@ -186,6 +194,7 @@ hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t 
   if (grad_entropy && !entropy) return fail(HPF_EINVAL, "entropy is required with grad_entropy");
   if (!rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
   if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
+  if (!words_aligned(labels, stats, grad_logprob, entropy, grad_entropy)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (overlap(Matrix{logits, rows, classes, ld, elem(dt)}, Matrix{dlogits, rows, classes, ldd, elem(dt)}) && (logits != dlogits || ld != ldd))
     return fail(HPF_EINVAL, "dlogits overlap the logits (they may be the same tensor)");
   const LogprobBackward a{logits, ld, labels, stats, grad_logprob, entropy, grad_entropy, dlogits, ldd, rows, classes};
@@ -207,6 +216,7 @@ hpf_status hpf_op_distill(hpf_dtype dtype, const void* logits, int64_t ld, const
   if (hard_weight > 0.f && !labels) return fail(HPF_EINVAL, "labels are required with hard_weight > 0");
   if (dlogits && !rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
   if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
+  if (!words_aligned(top_index, top_logit, labels, row_weight, loss)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (overlap(Matrix{logits, rows, classes, ld, elem(dt)}, Matrix{dlogits, rows, classes, ldd, elem(dt)})) return fail(HPF_EINVAL, "dlogits overlap the logits");
   st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
   if (st != HPF_OK) return st;

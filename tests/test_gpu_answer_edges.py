@@ -119,3 +119,26 @@ def test_entries_of_very_small_teacher_probability(env, mode, shape):
     assert torch.equal(loss, want[0])
     ref, dref, _ = distill64(torch, s, torch.full_like(index, -1), torch.zeros_like(logit), labels, 2.0, 1.0, None)
     check_distill(torch, mode, s, torch.full_like(index, -1), torch.zeros_like(logit), labels, 2.0, 1.0, None, loss, ds)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(3, 40, 24), (130, 200, 136), (1021, 257, 1000), (2304, 512, 4096), (700, 2600, 4104)])
+def test_weight_gradients_in_a_flat_buffer(env, mode, M, K, N):
+    """dw and db at any fp32 address of one buffer of gradients, written and added to; the numbers around them stay."""
+    hpf, torch = env
+    print(f"\n[case] flat gradients {M}x{K}x{N} {mode}", flush=True)
+    o = hpf.Ops(hpf.HPF_BF16 if mode == "bf16" else hpf.HPF_F32)
+    x, w, dy = randn(torch, 1, M, K).to(o.tdtype), randn(torch, 2, K, N), randn(torch, 3, M, N).to(o.tdtype)
+    weights = o.linear_weights(w)
+    _, dw, db = o.linear_backward(dy, x, weights)
+    for off in (0, 1, 2, 3):
+        flat = torch.full((off + K * N + N + 8,), 7.0, device="cuda")
+        vw, vb = flat[off:off + K * N].view(K, N), flat[off + K * N:off + K * N + N]
+        o.linear_backward(dy, x, weights, dw=vw, db=vb)
+        assert torch.equal(vw, dw) and torch.equal(vb, db)
+        assert bool((flat[:off] == 7).all()) and bool((flat[off + K * N + N:] == 7).all())
+        before = vw.clone()
+        o.linear_backward(dy, x, weights, dw=vw, db=vb, accumulate=True)
+        # one sum more, rounded once: 2^-24 of it (check mode: from double)
+        check(vw, before.double() + dw.double(), 2.0 ** -23 * before.double().abs() * 2, "dw added to")
+        assert bool((flat[:off] == 7).all()) and bool((flat[off + K * N + N:] == 7).all())
