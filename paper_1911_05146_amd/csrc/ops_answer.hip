@@ -36,6 +36,27 @@ bool overlap(const Matrix& a, const Matrix& b) {
   const int64_t at = ((d / e) % a.ld + a.ld) % a.ld;      // b's first column, counted from a's
   return at < a.cols || at + b.cols > a.ld;
 }
+// `count` numbers of 4 bytes, or `bytes`, in one piece
+Matrix words(const void* p, int64_t count) { return Matrix{p, 1, count, 0, 4}; }
+Matrix piece(const void* p, size_t bytes) { return Matrix{p, 1, (int64_t)bytes, 0, 1}; }
+// Whether an output shares an element with another output or with an input
+template <size_t O, size_t I>
+bool collide(const Matrix (&out)[O], const Matrix (&in)[I]) {
+  for (size_t i = 0; i < O; ++i) {
+    for (size_t j = i + 1; j < O; ++j)
+      if (overlap(out[i], out[j])) return true;
+    for (const Matrix& q : in)
+      if (overlap(out[i], q)) return true;
+  }
+  return false;
+}
+// The workspace is an output and holds nothing of the call's
+template <size_t N>
+bool workspace_apart(const void* workspace, size_t need, const Matrix (&of)[N]) {
+  for (const Matrix& q : of)
+    if (need && overlap(piece(workspace, need), q)) return false;
+  return true;
+}
 hpf_status launched(hipError_t e) { return e == hipSuccess ? HPF_OK : fail(HPF_EDEVICE, "launch failed: %s", hipGetErrorString(e)); }
 
 hpf_status linear_shape(hpf_dtype dtype, int32_t M, int32_t K, int32_t N, int& dt) {
@@ -46,6 +67,9 @@ hpf_status linear_shape(hpf_dtype dtype, int32_t M, int32_t K, int32_t N, int& d
   if ((int64_t)M * N > most || (int64_t)M * K > most || (int64_t)K * N > most)
     return fail(HPF_EUNSUPPORTED, "a matrix of more than 2^32 elements (%d, %d, %d)", M, K, N);
   return HPF_OK;
+}
+Matrix weights_of(int dt, const void* weights, int32_t K, int32_t N) {
+  return dt == DT_BF16 ? piece(weights, linear_packed_elems(K, N) * sizeof(bf16_t)) : words(weights, (int64_t)K * N);
 }
 hpf_status workspace_ok(const void* workspace, size_t bytes, size_t need) {
   if (!need) return HPF_OK;
@@ -97,14 +121,15 @@ hpf_status hpf_op_linear_forward(hpf_dtype dtype, const void* x, int64_t ldx, co
       (dt == DT_F32 && !element_aligned(weights, dt)))
     return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
-  const size_t e = elem(dt);
-  const Matrix in{x, M, K, ldx, e}, out{y, M, N, ldy, e}, kept{slope, M, N, N, e}, added{residual, M, N, ldr, e};
-  const Matrix w{weights, 1, dt == DT_BF16 ? (int64_t)hpf_op_linear_packed_bytes(K, N) : (int64_t)K * N * 4, 0, 1};
-  if (overlap(in, out) || overlap(in, kept) || overlap(out, kept) || overlap(w, out) || overlap(w, kept) || overlap(added, kept) ||
-      (overlap(added, out) && (residual != y || ldr != ldy)))
+  const size_t e = elem(dt), need = linear_workspace_bytes(dt, M, K, N);
+  const Matrix added{residual, M, N, ldr, e}, in[] = {{x, M, K, ldx, e}, weights_of(dt, weights, K, N), words(bias, N)},
+               out[] = {{y, M, N, ldy, e}, {slope, M, N, N, e}};
+  if (collide(out, in) || overlap(added, out[1]) || (overlap(added, out[0]) && (residual != y || ldr != ldy)))
     return fail(HPF_EINVAL, "an output overlaps another tensor (only residual and y may be the same)");
-  st = workspace_ok(workspace, workspace_bytes, linear_workspace_bytes(dt, M, K, N));
+  st = workspace_ok(workspace, workspace_bytes, need);
   if (st != HPF_OK) return st;
+  const Matrix all[] = {added, in[0], in[1], in[2], out[0], out[1]};
+  if (!workspace_apart(workspace, need, all)) return fail(HPF_EINVAL, "the workspace overlaps a tensor");
   const LinearForward a{x, ldx, weights, bias, residual, ldr, y, ldy, slope, M, K, N, activation};
   return launched(launch_linear_forward(dt, a, workspace, (hipStream_t)hip_stream));
 }
@@ -130,18 +155,13 @@ hpf_status hpf_op_linear_backward(hpf_dtype dtype, const void* dy, int64_t lddy,
       (dt == DT_F32 && !element_aligned(weights, dt)))
     return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (dx && dt == DT_BF16 && (uintptr_t)weights % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
-  const size_t e = elem(dt);
-  const Matrix in[] = {{dy, M, N, lddy, e}, {dw ? x : nullptr, M, K, ldx, e}, {slope, M, N, N, e},
-                       {dx ? weights : nullptr, 1, dt == DT_BF16 ? (int64_t)hpf_op_linear_packed_bytes(K, N) : (int64_t)K * N * 4, 0, 1}};
-  const Matrix out[] = {{dx, M, K, lddx, e}, {dw, 1, (int64_t)K * N, 0, 4}, {db, 1, N, 0, 4}};
-  for (int i = 0; i < 3; ++i) {
-    for (const Matrix& q : in)
-      if (overlap(out[i], q)) return fail(HPF_EINVAL, "an output overlaps an input");
-    for (int j = i + 1; j < 3; ++j)
-      if (overlap(out[i], out[j])) return fail(HPF_EINVAL, "two outputs overlap");
-  }
-  st = workspace_ok(workspace, workspace_bytes, linear_workspace_bytes(dt, M, K, N));
+  const size_t e = elem(dt), need = linear_workspace_bytes(dt, M, K, N);
+  const Matrix in[] = {{dy, M, N, lddy, e}, {dw ? x : nullptr, M, K, ldx, e}, {slope, M, N, N, e}, weights_of(dt, dx ? weights : nullptr, K, N)};
+  const Matrix out[] = {{dx, M, K, lddx, e}, words(dw, (int64_t)K * N), words(db, N)};
+  if (collide(out, in)) return fail(HPF_EINVAL, "an output overlaps another tensor");
+  st = workspace_ok(workspace, workspace_bytes, need);
   if (st != HPF_OK) return st;
+  if (!workspace_apart(workspace, need, in) || !workspace_apart(workspace, need, out)) return fail(HPF_EINVAL, "the workspace overlaps a tensor");
   const LinearBackward a{dy, lddy, x, ldx, weights, slope, dx, lddx, dw, db, accumulate, M, K, N};
   return launched(launch_linear_backward(dt, a, workspace, s));
 }
@@ -176,8 +196,15 @@ hpf_status hpf_op_logprob_forward(hpf_dtype dtype, const void* logits, int64_t l
   if (top && (!top_index || !top_logprob)) return fail(HPF_EINVAL, "top_index and top_logprob are required with a list");
   if (!words_aligned(labels, logprob, entropy, rank, stats, top_index, top_logprob)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if ((logprob || rank) && !labels) return fail(HPF_EINVAL, "labels are required for logprob and rank");
-  st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
+  const Matrix in[] = {{logits, rows, classes, ld, elem(dt)}, words(labels, rows)};
+  const int64_t entries = (int64_t)rows * top;
+  const Matrix out[] = {words(logprob, rows), words(entropy, rows), words(rank, rows), words(stats, 2 * (int64_t)rows), words(top ? top_index : nullptr, entries),
+                        words(top ? top_logprob : nullptr, entries)};
+  if (collide(out, in)) return fail(HPF_EINVAL, "an output overlaps another tensor");
+  const size_t need = logits_workspace_bytes(dt, rows, classes, top);
+  st = workspace_ok(workspace, workspace_bytes, need);
   if (st != HPF_OK) return st;
+  if (!workspace_apart(workspace, need, in) || !workspace_apart(workspace, need, out)) return fail(HPF_EINVAL, "the workspace overlaps a tensor");
   const LogprobForward a{logits, ld, labels, logprob, entropy, rank, stats, top_index, top_logprob, top, rows, classes};
   return launched(launch_logprob_forward(dt, a, workspace, (hipStream_t)hip_stream));
 }
@@ -197,6 +224,10 @@ hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t 
   if (!words_aligned(labels, stats, grad_logprob, entropy, grad_entropy)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if (overlap(Matrix{logits, rows, classes, ld, elem(dt)}, Matrix{dlogits, rows, classes, ldd, elem(dt)}) && (logits != dlogits || ld != ldd))
     return fail(HPF_EINVAL, "dlogits overlap the logits (they may be the same tensor)");
+  const Matrix in[] = {words(grad_logprob ? labels : nullptr, rows), words(stats, 2 * (int64_t)rows), words(grad_logprob, rows),
+                       words(grad_entropy ? entropy : nullptr, rows), words(grad_entropy, rows)};
+  const Matrix out[] = {{dlogits, rows, classes, ldd, elem(dt)}};
+  if (collide(out, in)) return fail(HPF_EINVAL, "dlogits overlap another tensor (only the logits may be the same)");
   const LogprobBackward a{logits, ld, labels, stats, grad_logprob, entropy, grad_entropy, dlogits, ldd, rows, classes};
   return launched(launch_logprob_backward(dt, a, (hipStream_t)hip_stream));
 }
@@ -217,9 +248,15 @@ hpf_status hpf_op_distill(hpf_dtype dtype, const void* logits, int64_t ld, const
   if (dlogits && !rows_ok(ldd, classes)) return fail(HPF_EINVAL, "row stride shorter than a row");
   if (!element_aligned(dlogits, dt)) return fail(HPF_EINVAL, "dlogits not aligned to their elements");
   if (!words_aligned(top_index, top_logit, labels, row_weight, loss)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
-  if (overlap(Matrix{logits, rows, classes, ld, elem(dt)}, Matrix{dlogits, rows, classes, ldd, elem(dt)})) return fail(HPF_EINVAL, "dlogits overlap the logits");
-  st = workspace_ok(workspace, workspace_bytes, logits_workspace_bytes(dt, rows, classes, top));
+  const int64_t entries = (int64_t)rows * top;
+  const Matrix in[] = {{logits, rows, classes, ld, elem(dt)}, words(top ? top_index : nullptr, entries), words(top ? top_logit : nullptr, entries),
+                       words(labels, rows), words(row_weight, rows)};
+  const Matrix out[] = {words(loss, rows), {dlogits, rows, classes, ldd, elem(dt)}};
+  if (collide(out, in)) return fail(HPF_EINVAL, "an output overlaps another tensor");
+  const size_t need = logits_workspace_bytes(dt, rows, classes, top);
+  st = workspace_ok(workspace, workspace_bytes, need);
   if (st != HPF_OK) return st;
+  if (!workspace_apart(workspace, need, in) || !workspace_apart(workspace, need, out)) return fail(HPF_EINVAL, "the workspace overlaps a tensor");
   const Distill a{logits, ld, top_index, top_logit, labels, row_weight, loss, dlogits, ldd, temperature, hard_weight, top, rows, classes};
   return launched(launch_distill(dt, a, workspace, (hipStream_t)hip_stream));
 }
