@@ -515,10 +515,13 @@ class Ops:
         return t.data_ptr(), step
 
     def _like_rows(self, t, ld):
-        """An empty matrix with t's shape and row stride: where the logits' rows start on 16 bytes their gradient's do too."""
+        """(empty matrix of t's shape, its row stride).  Rows lie apart as t's do, but for whole 128 bytes: where the logits' rows start on 16 or 128
+        bytes their gradient's do too, and logits that are a few columns of a wide matrix get a gradient of their own size."""
         rows, cols = t.shape
-        return self.torch.empty((rows, ld), dtype=self.tdtype, device=self.device)[:, :cols] if ld != cols else \
-            self.torch.empty((rows, cols), dtype=self.tdtype, device=self.device)
+        if ld != cols:
+            ld = cols + (ld - cols) % (128 // t.element_size())
+        d = self.torch.empty((rows, ld), dtype=self.tdtype, device=self.device)
+        return (d if ld == cols else d[:, :cols]), ld
 
     def _dense(self, name, t, shape, dtype):
         if t is None:
@@ -630,7 +633,7 @@ class Ops:
         lp, ld = self._rows("logits", logits)
         rows, classes = logits.shape
         f32 = torch.float32
-        d = out if out is not None else self._like_rows(logits, ld)
+        d = out if out is not None else self._like_rows(logits, ld)[0]
         dp, ldd = self._rows("out", d, (rows, classes))
         self._enqueue(hpf_op_logprob_backward, self.dt, lp, ld, self._labels(labels, rows), self._dense("stats", stats, (rows, 2), f32),
                       self._dense("grad_logprob", grad_logprob, (rows,), f32), self._dense("entropy", entropy, (rows,), f32),
@@ -647,11 +650,11 @@ class Ops:
         ti = self._dense("top_index", top_index, (rows, top), torch.int32)
         tl = self._dense("top_logit", top_logit, (rows, top), torch.float32)
         loss = torch.empty(rows, dtype=torch.float32, device=self.device)
-        d = self._like_rows(logits, ld) if gradient else None
+        d, ldd = self._like_rows(logits, ld) if gradient else (None, 0)
         n = hpf_op_logits_workspace_bytes(self.dt, rows, classes, top)
         ws, wsp = self._scratch(n)
         self._enqueue(hpf_op_distill, self.dt, lp, ld, ti, tl, top, self._labels(labels, rows), temperature, hard_weight,
-                      self._dense("row_weight", row_weight, (rows,), torch.float32), loss.data_ptr(), d.data_ptr() if gradient else 0, ld,
+                      self._dense("row_weight", row_weight, (rows,), torch.float32), loss.data_ptr(), d.data_ptr() if gradient else 0, ldd,
                       rows, classes, wsp, n)
         return loss, d
 

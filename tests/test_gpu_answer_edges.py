@@ -142,3 +142,30 @@ def test_weight_gradients_in_a_flat_buffer(env, mode, M, K, N):
         # one sum more, rounded once: 2^-24 of it (check mode: from double)
         check(vw, before.double() + dw.double(), 2.0 ** -23 * before.double().abs() * 2, "dw added to")
         assert bool((flat[:off] == 7).all()) and bool((flat[off + K * N + N:] == 7).all())
+
+
+@pytest.mark.parametrize("mode", ["bf16", "f32"])
+@pytest.mark.parametrize("at", [0, 3, 8])
+def test_gradients_of_a_few_columns_take_no_more_than_they_hold(env, mode, at):
+    """The gradient of logits that are a part of a much wider matrix has rows of its own, which start where the logits' do within 128 bytes."""
+    hpf, torch = env
+    o = hpf.Ops(hpf.HPF_BF16 if mode == "bf16" else hpf.HPF_F32)
+    rows, classes = 40, 1000
+    for width in (1 << 16, 1003, 1008, (1 << 15) + 3):
+        wide = randn(torch, 6, rows, width + 16).to(o.tdtype)[:, :width]
+        s = wide[:, at:at + classes] if at + classes <= width else wide[:, :classes]
+        labels = (torch.arange(rows, device="cuda") * 37 % classes).int()
+        r = o.logprob_forward(s, labels, 5)
+        one = torch.ones(rows, device="cuda")
+        d = o.logprob_backward(s, labels, r.stats, one)
+        loss, ds = o.distill(s, r.top_index, r.top_logprob, labels, hard_weight=0.5)
+        most = rows * (classes * s.element_size() + 128)
+        for g, want in ((d, o.logprob_backward(s.contiguous(), labels, r.stats, one)), (ds, None)):
+            held = g.untyped_storage().nbytes()
+            assert g.shape == s.shape and held <= most
+            phase = 128 // s.element_size()
+            assert g.stride(0) % phase == s.stride(0) % phase
+            if want is not None:
+                assert torch.equal(g, want)
+        dense = o.distill(s.contiguous(), r.top_index, r.top_logprob, labels, hard_weight=0.5)
+        assert bool(((loss - dense[0]).abs() <= 1e-6 * (1 + loss.abs())).all()) and bool(((ds.double() - dense[1].double()).abs() <= 2.0 ** -7 * ds.double().abs() + 1e-7).all())
