@@ -169,3 +169,23 @@ def test_gradients_of_a_few_columns_take_no_more_than_they_hold(env, mode, at):
                 assert torch.equal(g, want)
         dense = o.distill(s.contiguous(), r.top_index, r.top_logprob, labels, hard_weight=0.5)
         assert bool(((loss - dense[0]).abs() <= 1e-6 * (1 + loss.abs())).all()) and bool(((ds.double() - dense[1].double()).abs() <= 2.0 ** -7 * ds.double().abs() + 1e-7).all())
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+def test_tail_of_gelu(env, M):
+    """gelu(z) far below zero keeps the digits of its type: relative to its value, which falls to 2^-126 at -13.  The kernel's Phi(-|z|) is off by at
+    most 2^-12 of itself (the largest deviation of its polynomial), exp2 of z^2 / 2 by z^2 2^-23 <= 2^-15: together below 2^-11."""
+    hpf, torch = env
+    print(f"\n[case] gelu tail {M}", flush=True)
+    o = hpf.Ops(hpf.HPF_BF16)
+    z = torch.linspace(-13, 13, 4096, device="cuda").to(torch.bfloat16).float()
+    x = torch.ones(M, 1, device="cuda", dtype=torch.bfloat16)
+    y, slope = o.linear_forward(x, o.linear_weights(z[None].contiguous()), activation="gelu", slope=True)
+    z = z.double()
+    def below(v):                                        # torch.special.ndtr ends where 1 + erf rounds to 0, at -8.3
+        return 0.5 * torch.special.erfc(-v * 0.5 ** 0.5)
+    phi, density = below(z), torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    off = 2.0 ** -11 * below(-z.abs()) + torch.where(z > 0, 2.0 ** -22, 0.0)
+    ref, sref = z * phi, phi + z * density
+    check(y, ref.expand(M, -1), 2.0 ** -8 * 1.01 * ref.abs() + z.abs() * off + 2.0 ** -126, "y")
+    check(slope, sref.expand(M, -1), 2.0 ** -8 * 1.01 * sref.abs() + off + 2.0 ** -14 * z.abs() * density + 2.0 ** -126, "slope")
