@@ -89,10 +89,10 @@ size_t hpf_op_linear_packed_bytes(int32_t K, int32_t N) {
 }
 
 hpf_status hpf_op_linear_pack(const float* w, int32_t K, int32_t N, void* packed, size_t packed_bytes, void* hip_stream) {
-  if (!w || !packed) return fail(HPF_EINVAL, "null tensor");
   int dt;
   const hpf_status st = linear_shape(HPF_BF16, 0, K, N, dt);
   if (st != HPF_OK) return st;
+  if (!w || !packed) return fail(HPF_EINVAL, "null tensor");
   if (!words_aligned(w)) return fail(HPF_EINVAL, "tensor not aligned to its elements");
   if ((uintptr_t)packed % 256) return fail(HPF_EINVAL, "packed weights must be 256-byte aligned");
   const size_t need = hpf_op_linear_packed_bytes(K, N);

@@ -542,8 +542,8 @@ class Ops:
         torch = self.torch
         K, N = w.shape
         ptr = self._dense("w", w, (K, N), torch.float32)
-        if out is not None and (out.K, out.N, out.dtype) != (K, N, self.dt):
-            raise ValueError("out: weights of another shape or type")
+        if out is not None and ((out.K, out.N, out.dtype) != (K, N, self.dt) or not self._here(out.tensor)):
+            raise ValueError("out: weights of another shape, type or device")
         if self.dt == HPF_F32:
             if out is None:
                 return LinearWeights(K, N, self.dt, w, ptr)

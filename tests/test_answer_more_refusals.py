@@ -107,3 +107,16 @@ def test_what_lies_apart_is_not_refused(hpf):
     a, b, c, e, ti, tl = place(16), place(16), place(16), place(32), place(48), place(48)
     refused(hpf, hpf.HPF_ENOMEM, "workspace", hpf.hpf_op_logprob_forward, 1, s, n, labels, a, b, c, e, ti, tl, 3, 4, n, H, 1)
     refused(hpf, hpf.HPF_ENOMEM, "workspace", hpf.hpf_op_distill, 1, s, n, ti, tl, 3, labels, 1.0, 0.5, a, b, d, n, 4, n, H, 1)
+
+
+def test_weights_of_another_device_or_size(hpf):
+    """New weights go into an object of the same device (here the CPU stands in for one, whose memory is never touched); sizes beyond the limits are
+    said to be that."""
+    import torch
+    for dtype in (hpf.HPF_BF16, hpf.HPF_F32):
+        o = hpf.Ops(dtype, "cpu")
+        elsewhere = hpf.LinearWeights(16, 8, dtype, torch.zeros(16, 8, device="meta"), B)
+        with pytest.raises(ValueError, match="another shape, type or device"):
+            o.linear_weights(torch.zeros(16, 8), out=elsewhere)
+    refused(hpf, hpf.HPF_EUNSUPPORTED, "2^32", hpf.hpf_op_linear_pack, A, 1 << 20, 1 << 13, 0, 0)
+    refused(hpf, hpf.HPF_EUNSUPPORTED, "2^20", hpf.hpf_op_linear_pack, A, (1 << 20) + 1, 8, 0, 0)
