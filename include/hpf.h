@@ -449,7 +449,8 @@ hpf_status hpf_op_logprob_forward(hpf_dtype dtype, const void* logits, int64_t l
                                   int32_t rows, int32_t classes, void* workspace, size_t workspace_bytes, void* hip_stream);
 /* dlogits = grad_logprob * d logprob + grad_entropy * d entropy, from the stats and entropy of the forward call.  Either
  * gradient may be NULL (0); entropy is read with grad_entropy only, labels with grad_logprob only.  dlogits may be the
- * logits themselves. */
+ * logits themselves.  Fewer than 2^24 pieces of 16 KiB, counted row by row (in fp32 about 2^36 logits reach that; else
+ * HPF_EUNSUPPORTED). */
 hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* labels, const float* stats,
                                    const float* grad_logprob, const float* entropy, const float* grad_entropy, void* dlogits,
                                    int64_t ldd, int32_t rows, int32_t classes, void* hip_stream);

@@ -68,6 +68,13 @@ struct Distill {
 };
 size_t logits_workspace_bytes(int dt, int rows, int classes, int top);
 hipError_t launch_logprob_forward(int dt, const LogprobForward& a, void* workspace, hipStream_t stream);
+// 1024 16-byte units of a row, with the one that a row across a boundary has more: a work-group of 256 threads each.  A launch takes fewer than 2^32
+// threads.
+inline int64_t logprob_backward_pieces(size_t elem, int classes) {
+  const int64_t each = 16 / (int64_t)elem, units = (classes + each - 1) / each + 1;
+  return (units + 1023) / 1024;
+}
+constexpr int64_t LOGPROB_BACKWARD_MOST = (1 << 24) - 1;
 hipError_t launch_logprob_backward(int dt, const LogprobBackward& a, hipStream_t stream);
 hipError_t launch_distill(int dt, const Distill& a, void* workspace, hipStream_t stream);
 

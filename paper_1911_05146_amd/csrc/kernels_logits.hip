@@ -1226,8 +1226,7 @@ hipError_t logprob_forward(int dt, const LogprobForward& a, void* workspace, hip
 
 template <class T>
 hipError_t logprob_backward(const LogprobBackward& a, hipStream_t s) {
-  const long units = (a.classes + 16 / (long)sizeof(T) - 1) / (16 / (long)sizeof(T)) + 1;
-  const unsigned per_row = (unsigned)((units + 1023) / 1024);
+  const unsigned per_row = (unsigned)logprob_backward_pieces(sizeof(T), a.classes);
   k_logprob_backward<T><<<(unsigned)a.rows * per_row, 256, 0, s>>>(a, per_row);
   return hipGetLastError();
 }

@@ -216,6 +216,8 @@ hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t 
   hpf_status st = logits_shape(dtype, logits, ld, 0, rows, classes, dt);
   if (st != HPF_OK) return st;
   if (rows == 0) return HPF_OK;
+  if (rows * logprob_backward_pieces(elem(dt), classes) > LOGPROB_BACKWARD_MOST)
+    return fail(HPF_EUNSUPPORTED, "a gradient of 2^24 pieces of 16 KiB or more (%d rows of %d classes)", rows, classes);
   if (!stats || !dlogits) return fail(HPF_EINVAL, "stats and dlogits are required");
   if (grad_logprob && !labels) return fail(HPF_EINVAL, "labels are required with grad_logprob");
   if (grad_entropy && !entropy) return fail(HPF_EINVAL, "entropy is required with grad_entropy");

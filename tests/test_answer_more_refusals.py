@@ -120,3 +120,11 @@ def test_weights_of_another_device_or_size(hpf):
             o.linear_weights(torch.zeros(16, 8), out=elsewhere)
     refused(hpf, hpf.HPF_EUNSUPPORTED, "2^32", hpf.hpf_op_linear_pack, A, 1 << 20, 1 << 13, 0, 0)
     refused(hpf, hpf.HPF_EUNSUPPORTED, "2^20", hpf.hpf_op_linear_pack, A, (1 << 20) + 1, 8, 0, 0)
+
+
+def test_gradients_beyond_a_launch(hpf):
+    """2^24 work-groups of 256 threads and more are no launch: fp32 logits whose rows have 2^24 pieces of 4096 in all."""
+    for rows, classes in ((1 << 21, 1 << 15), (1 << 21, 7 * 4096 - 2), (256, 1 << 28), (1 << 12, 1 << 24)):
+        refused(hpf, hpf.HPF_EUNSUPPORTED, "2^24", lambda: logprob_gradient(hpf, rows=rows, classes=classes, dtype=hpf.HPF_F32))
+    for rows, classes, dtype in ((1 << 21, 7 * 4096 - 4, hpf.HPF_F32), (1 << 21, 1 << 15, hpf.HPF_BF16), (256, 1 << 28, hpf.HPF_BF16)):
+        refused(hpf, hpf.HPF_EINVAL, "stats", lambda: logprob_gradient(hpf, rows=rows, classes=classes, dtype=dtype, stats=0))     # refused for another reason
