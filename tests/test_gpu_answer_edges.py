@@ -189,3 +189,19 @@ def test_tail_of_gelu(env, M):
     ref, sref = z * phi, phi + z * density
     check(y, ref.expand(M, -1), 2.0 ** -8 * 1.01 * ref.abs() + z.abs() * off + 2.0 ** -126, "y")
     check(slope, sref.expand(M, -1), 2.0 ** -8 * 1.01 * sref.abs() + off + 2.0 ** -14 * z.abs() * density + 2.0 ** -126, "slope")
+
+
+@pytest.mark.parametrize("shape", [(6, 1000), (1100, 2052), (200, 20001), (140, 65537), (2, 70001)], ids=lambda s: "x".join(map(str, s)))
+def test_lists_of_logits_far_from_zero(env, shape):
+    """A common offset that leaves the logits a few hundred or thousand steps of fp32 apart: many distinct values within what a coarse bound tells
+    apart, and many equal ones."""
+    from test_gpu_logits import check_forward
+    hpf, torch = env
+    print(f"\n[case] far from zero {shape}", flush=True)
+    o = hpf.Ops(hpf.HPF_F32)
+    rows, classes = shape
+    labels = (torch.arange(rows, device="cuda") * 7919 % classes).int()
+    for offset in (1e4, -1e5):
+        s = randn(torch, 7, rows, classes) * 2.5 + offset
+        for top in (5, 64):
+            check_forward(torch, s, labels, top, o.logprob_forward(s, labels, top))
