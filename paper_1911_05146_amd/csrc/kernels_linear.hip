@@ -552,7 +552,7 @@ __global__ __launch_bounds__(512) void k_linear_few(Product p, int steps_per_spl
   finish8<OUT>(p, m, n, v, blockIdx.y, ahead<OUT>(p, n), residual8<OUT>(p, m, n));
 }
 
-// y or the sum from the shares of a split contraction (4.4 us of the 14 at 128 x 4096 x 4096, four shares)
+// y or the sum from the shares of a split contraction (4.3 us of the 14 at 128 x 4096 x 4096, two shares of 128 tiles)
 template <int OUT>
 __global__ __launch_bounds__(256) void k_linear_join(Product p, const float* __restrict__ slabs, int splits) {
   const int units = (p.N + 7) / 8;
@@ -670,7 +670,8 @@ __global__ __launch_bounds__(1024) void k_linear_db_join(const float* __restrict
   }
 }
 
-// packed copies of w: blocks of 64 x 64 through LDS (4096 x 4096: 30 us, 4.5 TB/s read and written)
+// packed copies of w: blocks of 64 x 64 through LDS, stored 2 bytes at a time (4096 x 4096, 134 MB read and written: 37 us from memory, 3.6 TB/s; 23
+// where w is in a cache from the call before)
 __global__ __launch_bounds__(256) void k_linear_pack(const float* __restrict__ w, bf16_t* __restrict__ packed, int K, int N, int Kp, int Np) {
   __shared__ float tile[64][65];
   const int k0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
@@ -689,7 +690,7 @@ __global__ __launch_bounds__(256) void k_linear_pack(const float* __restrict__ w
   }
 }
 
-// fp32: dz, and its column sums, 64 per work-group
+// fp32: dz = dy * slope, rounded once
 __global__ __launch_bounds__(256) void k_linear_dz_f32(const float* __restrict__ dy, long lddy, const float* __restrict__ slope, float* __restrict__ dz, int M, int N) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)M * N; i += (size_t)gridDim.x * 256) {
     const size_t m = i / N, n = i - m * N;
@@ -697,6 +698,7 @@ __global__ __launch_bounds__(256) void k_linear_dz_f32(const float* __restrict__
   }
 }
 
+// fp32: column sums of dz in double, 64 columns per work-group: 16 shares of the rows, then their sums
 __global__ __launch_bounds__(1024) void k_linear_db_f32(const float* __restrict__ dz, long ld, float* __restrict__ db, int accumulate, int M, int N) {
   __shared__ double part[16][64];
   const int c = threadIdx.x & 63, g = threadIdx.x >> 6, n = blockIdx.x * 64 + c;

@@ -538,7 +538,8 @@ class Ops:
         return t, (t.data_ptr() + 255) // 256 * 256
 
     def linear_weights(self, w, out=None):
-        """w: fp32 [K, N].  out: the object of an earlier call, which gets the new weights in place."""
+        """w: fp32 [K, N].  out: the object of an earlier call, which gets the new weights in place (check mode: it then stands for this w, which
+        it does not copy; a captured call keeps the one that it was captured with)."""
         torch = self.torch
         K, N = w.shape
         ptr = self._dense("w", w, (K, N), torch.float32)
