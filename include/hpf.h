@@ -461,7 +461,7 @@ hpf_status hpf_op_logprob_backward(hpf_dtype dtype, const void* logits, int64_t 
  *   loss[row] = (1 - hard_weight) * temperature^2 * sum_j p_j (log p_j - log q_j) + hard_weight * (-log softmax(logits)[label])
  *   dlogits[row] = row_weight[row] * d loss[row] / d logits[row]
  * in one call.  A row without entries or without label has no such term.  row_weight NULL: 1.  dlogits NULL: the loss alone.
- * labels may be NULL if hard_weight is 0; with hard_weight 1 only the list's indices are looked at.  temperature in [1e-4, 1e4], hard_weight in [0, 1]. */
+ * labels may be NULL if hard_weight is 0; with hard_weight 1 the list has no say but that of a bad index.  temperature in [1e-4, 1e4], hard_weight in [0, 1]. */
 hpf_status hpf_op_distill(hpf_dtype dtype, const void* logits, int64_t ld, const int32_t* top_index, const float* top_logit,
                           int32_t top, const int32_t* labels, float temperature, float hard_weight, const float* row_weight,
                           float* loss, void* dlogits, int64_t ldd, int32_t rows, int32_t classes, void* workspace,
